@@ -18,6 +18,10 @@
  *                       done loop of Sec. 3.2)
  *   sled_prefill        (beyond the step) a request's prompt through the same kernels into
  *                       its cache
+ *   sled_verify_tree    (beyond the step) the step for devices that draft trees instead of
+ *                       chains, with sled_accept_tree and sled_tree_commit
+ *   sled_kv_evict       (beyond the step) a request's cache cut down to the tokens that
+ *                       attention uses
  *
  * General rules
  *   - Plain C.  Every function returns SLED_OK (0) or a negative error code; nothing
@@ -172,7 +176,8 @@ SLED_API int sled_kvpool_destroy(sled_kvpool* p);
  * (1) accept_len == NULL: append n_tokens[i] tokens of externally produced K/V to request
  *     req_ids[i].  k_src[i] and v_src[i] (host arrays of B dev pointers) each point to
  *     [n_layers, n_tokens[i], n_kv_heads, head_dim] in the model dtype; K already rotated
- *     for positions L_i .. L_i + n_tokens[i] - 1.  L_i grows by n_tokens[i].
+ *     for positions L_i .. L_i + n_tokens[i] - 1 (after an eviction: from the text's position on,
+ *     sled_kvpool_positions).  L_i grows by n_tokens[i].
  *
  * (2) accept_len != NULL (dev, B int32, as written by sled_accept): commit the K/V that the
  *     last sled_verify_batch staged for these requests: the pending token and the first
@@ -332,6 +337,128 @@ SLED_API int sled_accept_sparse(int B, const int* k /*host*/, int vocab, float t
  * Errors: SLED_EINVAL. */
 SLED_API int sled_row_confidence(int T, int vocab, float temperature, const float* logits /*dev*/, float* conf /*dev out*/,
                         int32_t* top /*dev out or NULL*/, void* workspace /*dev*/, size_t workspace_bytes, void* stream);
+
+/* ---- trees of drafts --------------------------------------------------------------- */
+
+/* A device may draft a tree instead of a chain: several guesses for a position, each continued on its own.  A request's
+ * tree has 1 to SLED_TREE_MAX nodes, packed request-major like the rows of a chain; node 0 is the pending token, node j >= 1
+ * drafts the token that follows node parent[j], 0 <= parent[j] < j (parent[0] is not looked at).  A node sees the whole
+ * context, its ancestors and itself, and sits as many positions behind the context as it has ancestors.  The K/V of node j
+ * is staged in the tail slot L_i + j.  A chain is the tree with parent[j] = j - 1.
+ *
+ * A step over trees: sled_verify_tree, sled_accept_tree, sled_tree_commit.  Programs that run their own projections around
+ * the library's cache call sled_tree_begin once and sled_tree_attention per layer in place of sled_verify_tree. */
+#define SLED_TREE_MAX 64
+
+/* Bytes of scratch sled_tree_begin needs for batches of at most B_max trees with T_max nodes together on top of at most
+ * ctx_tokens_max tokens (sum of L_i + n_i, by the library's bounds on L_i: between a commit and the arrival of its exact
+ * lengths, every staged node counts). */
+SLED_API size_t sled_tree_workspace_bytes(const sled_model* m, int B_max, int T_max, int64_t ctx_tokens_max);
+
+/* Plans the attention of a batch of trees (which nodes see which, how contexts are cut into work items) and reserves
+ * the pages of their nodes.
+ *   req_ids[B], n_nodes[B], parent[T]  host; T = sum of n_nodes; a request may appear only once
+ *   workspace                          dev scratch, 256-byte aligned; the plan lives in it until the requests' next
+ *                                      commit, append, verify, prefill, eviction or close, or the pool's next
+ *                                      sled_tree_begin or sled_verify_tree
+ * What an earlier step staged for these requests is dropped.  Cannot be captured into a graph (the calls that use the
+ * plan, sled_tree_attention and sled_tree_mass, can; replays then use the plan the workspace holds at that time, on
+ * unchanged requests).
+ * Errors: SLED_EINVAL (bad tree, unknown or duplicate request, small workspace), SLED_ENOMEM, SLED_ESTATE (capture). */
+SLED_API int sled_tree_begin(sled_kvpool* p, int B, const int* req_ids /*host*/, const int* n_nodes /*host*/, const int* parent /*host*/,
+                    void* workspace /*dev*/, size_t workspace_bytes, void* stream);
+
+/* Attention of the planned trees' nodes on one layer's cache, and their K/V into the cache.
+ *   q[T] rows of [n_q_heads, head_dim], k[T] and v[T] rows of [n_kv_heads, head_dim]: dev, model dtype, q and k already
+ *        rotated; rows q_stride, k_stride, v_stride elements apart (so they may be parts of one matrix), 16-byte aligned
+ *   out  dev, model dtype, [T, n_q_heads, head_dim], 16-byte aligned:  softmax(q K^T / sqrt(head_dim)) V over what a node sees
+ *   lse  dev float32 [T, n_q_heads] or NULL: natural logarithm of the softmax's denominator
+ *   workspace  the one sled_tree_begin was given
+ * Softmax and sums in float32; a bf16 model's weights enter the product with V with 16 significant bits, the result is
+ * rounded once.  Keys and values of a node do not reach nodes that do not see it, not even where they are not finite.
+ * out and lse must not overlap the inputs.  Results do not depend on the other requests of the batch but for the order of float32 sums over split contexts
+ * (not even that for batch-invariant models).  Errors: SLED_EINVAL, SLED_ESTATE (no plan). */
+SLED_API int sled_tree_attention(sled_kvpool* p, int layer, const void* q /*dev*/, int64_t q_stride, const void* k /*dev*/, int64_t k_stride,
+                        const void* v /*dev*/, int64_t v_stride, void* out /*dev out*/, float* lse /*dev out or NULL*/,
+                        void* workspace /*dev*/, void* stream);
+
+/* Adds up what weight each cached token got on one layer: mass[token] += sum over the nodes of the request's tree and the query
+ * heads of a kv head of softmax(q K^T / sqrt(head_dim))[token].  For sled_kv_evict.  Comes after sled_tree_attention of that layer,
+ * with its q and the lse it returned.
+ *   mass  dev float32 [max_requests][n_layers][n_kv_heads][mass_cap], the row of a request by its id; mass_cap at least the
+ *         library's bound of L_i + n_i.  Zero a request's rows when it is opened; at and behind position L they are zero
+ *         whenever no tree is staged.  A node's own slot gets its mass (set, not added to), which sled_tree_commit moves with the node.
+ * One sum in a fixed order per token: no atomics.  Errors: SLED_EINVAL, SLED_ESTATE (no plan). */
+SLED_API int sled_tree_mass(sled_kvpool* p, int layer, const void* q /*dev*/, int64_t q_stride, const float* lse /*dev*/, float* mass /*dev inout*/,
+                   int mass_cap, void* workspace /*dev*/, void* stream);
+
+/* Commits the accepted paths: the pending token and the first accept_len[i] nodes of path[i] become context, in that order --
+ * their K/V (and, with mass, their mass) move together into positions L_i .. L_i + accept_len[i], and L_i grows by
+ * accept_len[i] + 1.
+ *   accept_len[B], path[B][SLED_TREE_MAX]  dev int32, as written by sled_accept_tree.  A path ends early where it does
+ *                                          not ascend within 1 .. n_i - 1
+ *   mass     dev or NULL, as in sled_tree_mass; the mass of nodes that are not on the path is cleared
+ * The requests must be among those of the last sled_verify_tree or sled_tree_begin, each at most once; several calls may commit
+ * them.  Cannot be captured.  Errors: SLED_EINVAL, SLED_ESTATE. */
+SLED_API int sled_tree_commit(sled_kvpool* p, int B, const int* req_ids /*host*/, const int32_t* accept_len /*dev*/, const int32_t* path /*dev*/,
+                     float* mass /*dev or NULL*/, int mass_cap, void* stream);
+
+/* sled_verify_batch for trees: target logits of every node, node j's row being the distribution of the token that follows it.
+ *   tokens[T]        dev int32, packed by request, in the order of the nodes; ids outside [0, vocab) are clamped into range
+ *   logits[T, vocab] dev float32 out
+ *   mass             dev or NULL: sled_tree_mass on every layer
+ *   workspace        dev scratch of at least sled_verify_tree_workspace_bytes(...) bytes, 256-byte aligned
+ * Stages the nodes' K/V without changing L_i, like sled_verify_batch; commit with sled_tree_commit.  k_max does not bound trees.
+ * A retry of a step that has added to mass adds to it again.  Cannot be captured.
+ * Errors: SLED_EINVAL, SLED_ENOMEM, SLED_ESTATE (capture). */
+SLED_API size_t sled_verify_tree_workspace_bytes(const sled_model* m, int B_max, int T_max, int64_t ctx_tokens_max);
+SLED_API int sled_verify_tree(sled_model* m, sled_kvpool* p, int B, const int* req_ids /*host*/, const int* n_nodes /*host*/, const int* parent /*host*/,
+                     const int32_t* tokens /*dev*/, float* logits /*dev out*/, float* mass /*dev or NULL*/, int mass_cap,
+                     void* workspace /*dev*/, size_t workspace_bytes, void* stream);
+
+/* Acceptance over trees, on given logits.  The walk starts at node 0.  At node c the target names a token:
+ *   mode SLED_GREEDY  the argmax of c's row (lowest id on ties);
+ *   mode SLED_SAMPLE  a draw from softmax(row / temperature): the smallest id whose cumulative probability exceeds u[c], in float64.
+ * The lowest child of c that drafted this token is accepted and becomes c; if there is none, the walk ends and the token is the
+ * answer.  Every token is thus the target's own choice, however the tree was drafted: greedy text equals plain decoding, sampled
+ * text has the target's distribution (the drafter's distributions are not needed).
+ *   n_nodes[B], parent[T]  host
+ *   logits[T, V]           dev float32, finite or -infinity, at least one finite per row;  tokens[T] dev int32
+ *   u[T]                   dev float32 uniforms in [0, 1), one per node (SLED_SAMPLE only, else may be NULL)
+ *   accept_len[B]          dev int32 out: accepted drafts;  out_token[B]  dev int32 out: the token that follows them
+ *   path[B][SLED_TREE_MAX] dev int32 out: the accepted nodes in order, -1 behind them
+ *   workspace              dev scratch of at least sled_accept_tree_workspace_bytes(B, T, vocab) bytes, 256-byte aligned
+ * Allocates nothing and can be captured (the trees' shape is part of the captured launch).  B <= 1024.  Errors: SLED_EINVAL. */
+SLED_API size_t sled_accept_tree_workspace_bytes(int B, int T, int vocab);
+SLED_API int sled_accept_tree(int mode, int B, const int* n_nodes /*host*/, const int* parent /*host*/, int vocab, float temperature,
+                     const float* logits /*dev*/, const int32_t* tokens /*dev*/, const float* u /*dev or NULL*/,
+                     int32_t* accept_len /*dev out*/, int32_t* path /*dev out*/, int32_t* out_token /*dev out*/,
+                     void* workspace /*dev*/, size_t workspace_bytes, void* stream);
+
+/* ---- eviction ----------------------------------------------------------------------- */
+
+/* Cuts the cache of requests down to keep[i] tokens, by the weight that attention gave them (sled_tree_mass).  Per layer and kv
+ * head are kept: the first n_first and the last n_recent tokens, and of those between the keep[i] - n_first - n_recent with
+ * the largest mass (equal masses: the lower position).  The kept tokens' K/V and mass move together in ascending order and L_i
+ * becomes keep[i]; a request of at most keep[i] tokens stays as it is.  Heads keep different tokens, so afterwards a position of the
+ * cache no longer stands for one token of the text.  Tokens to come keep the text's positions: their rotary angle follows
+ * the number of tokens committed in all (sled_kvpool_positions), which K appended from elsewhere has to be rotated for too.
+ *   dst_ids  host or NULL.  NULL: in place; pages that are no longer needed go back to the pool, and a step that is staged but not committed
+ *            is dropped.  Otherwise B open, empty requests that take the kept tokens, and the sources stay as they are
+ *            (one prompt's cache cut to the budgets of several devices)
+ *   keep[B]  host, >= 1 and >= n_first + n_recent
+ *   mass     dev float32, as in sled_tree_mass, finite; a destination's row takes the kept masses.  Zero behind the kept tokens (up to the old
+ *            length)
+ *   workspace  dev scratch of at least sled_kv_evict_workspace_bytes(m, B, largest keep) bytes, 256-byte aligned
+ * Cannot be captured.  Errors: SLED_EINVAL, SLED_ENOMEM (no page for a destination), SLED_ESTATE (destination not empty; capture). */
+SLED_API size_t sled_kv_evict_workspace_bytes(const sled_model* m, int B_max, int keep_max);
+SLED_API int sled_kv_evict(sled_kvpool* p, int B, const int* req_ids /*host*/, const int* dst_ids /*host or NULL*/, const int* keep /*host*/,
+                  int n_first, int n_recent, float* mass /*dev inout*/, int mass_cap, void* workspace /*dev*/, size_t workspace_bytes,
+                  void* stream);
+
+/* Where the requests' texts have got to: the position that the next token's K is rotated for, that is L_i and the tokens
+ * evicted so far.  Waits for `stream`, like sled_kvpool_lengths.  Errors: SLED_EINVAL. */
+SLED_API int sled_kvpool_positions(sled_kvpool* p, int B, const int* req_ids /*host*/, int* positions /*host out*/, void* stream);
 
 /* ---- kernel timing (measurement aid) ---------------------------------------------- */
 

@@ -9,7 +9,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libsled.so")
-SOURCES = ["api.hip", "gemm.hip", "rowops.hip", "attention.hip", "accept.hip"]
+SOURCES = ["api.hip", "gemm.hip", "rowops.hip", "attention.hip", "accept.hip", "tree.hip", "evict.hip", "accept_tree.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 
@@ -28,7 +28,7 @@ def _compile(src: str) -> str:
 
 def build(verbose: bool = True) -> str:
     os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
-    with ThreadPoolExecutor(max_workers=min(5, os.cpu_count() or 1)) as ex:
+    with ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 1)) as ex:
         objs = list(ex.map(_compile, SOURCES))
     cmd = ["hipcc", "-shared", "-fPIC", "--offload-arch=gfx950", *objs, "-o", OUT]
     r = subprocess.run(cmd, capture_output=True, text=True)

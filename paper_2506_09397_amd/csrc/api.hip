@@ -7,6 +7,7 @@
 #include <stdio.h>
 #include <string.h>
 #include <algorithm>
+#include <exception>
 #include <new>
 
 // ------------------------------------------------------------------------------------------ errors
@@ -352,7 +353,7 @@ extern "C" int sled_kvpool_create(const sled_model* m, int64_t n_pages, int max_
     p->max_requests = max_requests;
     p->page_head_elems = (size_t)16 * m->s.head_dim;
     p->k_pool = p->v_pool = nullptr;
-    p->len_dev = nullptr;
+    p->len_dev = p->shift_dev = nullptr;
     for (int i = 0; i < sled_kvpool::RING; i++) p->slot[i] = sled_stage_slot{nullptr, nullptr, nullptr, false};
     p->stage_cap = 0;
     p->stage_next = 0;
@@ -367,10 +368,13 @@ extern "C" int sled_kvpool_create(const sled_model* m, int64_t n_pages, int max_
     if ((e = hipMalloc(&p->v_pool, bytes)) != hipSuccess) return fail(SLED_ENOMEM, "hipMalloc(V pool)", e);
     if ((e = hipMalloc(reinterpret_cast<void**>(&p->len_dev), max_requests * sizeof(int32_t))) != hipSuccess)
         return fail(SLED_ENOMEM, "hipMalloc(lengths)", e);
+    if ((e = hipMalloc(reinterpret_cast<void**>(&p->shift_dev), max_requests * sizeof(int32_t))) != hipSuccess)
+        return fail(SLED_ENOMEM, "hipMalloc(lengths)", e);
     // pages never written hold zeros (read only under the mask, but keep them finite)
     if ((e = hipMemset(p->k_pool, 0, bytes)) != hipSuccess) return fail(SLED_EHIP, "hipMemset", e);
     if ((e = hipMemset(p->v_pool, 0, bytes)) != hipSuccess) return fail(SLED_EHIP, "hipMemset", e);
     if ((e = hipMemset(p->len_dev, 0, max_requests * sizeof(int32_t))) != hipSuccess) return fail(SLED_EHIP, "hipMemset", e);
+    if ((e = hipMemset(p->shift_dev, 0, max_requests * sizeof(int32_t))) != hipSuccess) return fail(SLED_EHIP, "hipMemset", e);
     p->stage_cap = 1 << 16;
     for (int i = 0; i < sled_kvpool::RING; i++) {
         if (slot_alloc(p->slot[i], p->stage_cap) != SLED_OK) {
@@ -409,6 +413,7 @@ extern "C" int sled_kvpool_destroy(sled_kvpool* p) {
     if (p->k_pool) (void)hipFree(p->k_pool);
     if (p->v_pool) (void)hipFree(p->v_pool);
     if (p->len_dev) (void)hipFree(p->len_dev);
+    if (p->shift_dev) (void)hipFree(p->shift_dev);
     delete p;
     return SLED_OK;
 }
@@ -431,6 +436,16 @@ extern "C" int sled_kvpool_open(sled_kvpool* p, int* req_id) {
     SLED_FAIL(SLED_ENOMEM, "sled_kvpool_open: all %d request slots are in use", p->max_requests);
 }
 
+// A request's length or pages change, or its tail slots are overwritten: the trees at hand cannot be attended to any more, and this request's
+// cannot be committed (the others' can).
+static void leave_tree(sled_kvpool* p, int req) {
+    auto& t = p->tree;
+    const auto it = std::find(t.reqs.begin(), t.reqs.end(), req);
+    if (it == t.reqs.end()) return;
+    t.reqs.erase(it);
+    t.valid = false;
+}
+
 extern "C" int sled_kvpool_close(sled_kvpool* p, int req_id) {
     if (!p || req_id < 0 || req_id >= p->max_requests || !p->reqs[req_id].open)
         SLED_FAIL(SLED_EINVAL, "sled_kvpool_close: request %d is not open", req_id);
@@ -442,6 +457,7 @@ extern "C" int sled_kvpool_close(sled_kvpool* p, int req_id) {
     p->reqs[req_id] = sled_request();
     p->reqs[req_id].gen = gen;
     p->last_batch.erase(std::remove(p->last_batch.begin(), p->last_batch.end(), req_id), p->last_batch.end());
+    leave_tree(p, req_id);
     return SLED_OK;
 }
 
@@ -482,7 +498,7 @@ static int reset_fresh_lengths(sled_kvpool* p, int B, const int* req_ids, hipStr
     std::vector<int> ids;
     for (int i = 0; i < B; i++)
         if (p->reqs[req_ids[i]].fresh) ids.push_back(req_ids[i]);
-    const int rc = sled_launch_len_zero(p->len_dev, ids.data(), (int)ids.size(), st);
+    const int rc = sled_launch_len_zero(p->len_dev, p->shift_dev, ids.data(), (int)ids.size(), st);
     if (rc != SLED_OK) return rc;
     for (int r : ids) p->reqs[r].fresh = false;
     return SLED_OK;
@@ -566,7 +582,7 @@ extern "C" int sled_kv_append(sled_kvpool* p, int B, const int* req_ids, const i
         if ((rc = stage_acquire(p, B, &sl)) != SLED_OK) return rc;
         for (int i = 0; i < B; i++) sl->host[i] = req_ids[i];
         SLED_HIP(hipMemcpyAsync(sl->dev, sl->host, B * sizeof(int32_t), hipMemcpyHostToDevice, st));
-        if ((rc = sled_launch_len_add(p->len_dev, sl->dev, nullptr, nullptr, accept_len, B, st)) != SLED_OK) return rc;
+        if ((rc = sled_launch_len_add(p->len_dev, p->shift_dev, sl->dev, nullptr, nullptr, accept_len, B, st)) != SLED_OK) return rc;
         if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
         for (int i = 0; i < B; i++) {
             sled_request& rq = p->reqs[req_ids[i]];
@@ -604,13 +620,14 @@ extern "C" int sled_kv_append(sled_kvpool* p, int B, const int* req_ids, const i
     }
     SLED_HIP(hipMemcpyAsync(sl->dev, sl->host, off * sizeof(int32_t), hipMemcpyHostToDevice, st));
     if ((rc = sled_launch_kv_ingest(m, p, pieces.data(), (int)pieces.size(), st)) != SLED_OK) return rc;
-    if ((rc = sled_launch_len_add(p->len_dev, sl->dev, sl->dev + B, sl->dev + 2 * B, nullptr, B, st)) != SLED_OK) return rc;
+    if ((rc = sled_launch_len_add(p->len_dev, p->shift_dev, sl->dev, sl->dev + B, sl->dev + 2 * B, nullptr, B, st)) != SLED_OK) return rc;
     if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
     for (int i = 0; i < B; i++) {
         sled_request& rq = p->reqs[req_ids[i]];
         rq.fresh = false;
         rq.len_ub += n_tokens[i];
         rq.added += n_tokens[i];
+        leave_tree(p, req_ids[i]);
         rq.staged = -1;   // rows staged by an uncommitted verify are overwritten: nothing of this request is left to commit
     }
     return SLED_OK;
@@ -794,6 +811,16 @@ extern "C" size_t sled_verify_workspace_bytes(const sled_model* m, int B_max, in
 
 namespace {
 
+// what a step over trees needs beside the blocks' rows
+struct tree_step {
+    const sled_tree_plan* plan;
+    const int* depth;        // [T] host
+    void *k, *v;             // [T][n_kv_heads * head_dim] scratch
+    float* lse;              // [T][n_q_heads] scratch
+    float* mass;             // or nullptr
+    int cap;
+};
+
 // One row block of a step: `rows` consecutive tokens of request `req`, the first of them `pos0` positions behind
 // the request's committed length.  A verification request is one block (pos0 = 0, rows = k + 1); a prompt is cut
 // into blocks of at most k_max + 1 rows that follow one another.
@@ -804,8 +831,9 @@ struct step_entry {
 // The forward pass over the packed rows of `ent` on top of the cached contexts: new K/V go to the requests' pages
 // (nothing is committed here), and the logits of all rows go to logits_all [T, vocab], or those of the single row
 // one_row to logits_one [vocab], or nowhere.
+// tr: the blocks are trees, attended to by the plan that sled_tree_begin's part of the work has made.
 int run_forward(sled_model* m, sled_kvpool* p, const std::vector<step_entry>& ent, const int32_t* tokens, float* logits_all,
-                int one_row, float* logits_one, void* workspace, size_t workspace_bytes, hipStream_t st, const char* who) {
+                int one_row, float* logits_one, void* workspace, size_t workspace_bytes, hipStream_t st, const char* who, const tree_step* tr = nullptr) {
     const sled_shape& s = m->s;
     const int B = (int)ent.size();
     const int Hkv = s.n_kv_heads, G = s.n_q_heads / Hkv;
@@ -833,11 +861,12 @@ int run_forward(sled_model* m, sled_kvpool* p, const std::vector<step_entry>& en
     std::vector<int> order(B);
     for (int i = 0; i < B; i++) order[i] = i;
     if (!m->batch_invariant) std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return np_all[a] > np_all[b]; });
-    const int tgt = m->batch_invariant ? 0 : attn_pages_per_item(np_all, order, Hkv);
-    std::vector<int32_t> work;
+    const int tgt = m->batch_invariant || tr ? 0 : attn_pages_per_item(np_all, order, Hkv);
+    std::vector<int32_t> work;   // (empty for trees)
     // first item of (block, kv head) and how many there are, Hkv places apart: the items of a pair all read the same q rows, and with a
     // multiple of eight heads they run on one XCD and share its L2
     std::vector<int32_t> cu_work(2 * B * Hkv);
+    if (tr) order.clear();
     for (int i : order) {
         const int np = np_all[i];
         const int chunk = m->batch_invariant ? SLED_FIXED_CHUNK_PAGES : attn_chunk(np, tgt);
@@ -857,17 +886,17 @@ int run_forward(sled_model* m, sled_kvpool* p, const std::vector<step_entry>& en
     const int n_work = (int)(work.size() / 4);
     // query tiles follow the longest block of the batch -- or, batch-invariant, of the model: the tile count sets
     // the number of page groups a workgroup splits its pages over
-    const int QT = std::max(1, ceil_div(G * (m->batch_invariant ? s.k_max + 1 : nmax), 16));
+    const int QT = tr ? 1 : std::max(1, ceil_div(G * (m->batch_invariant ? s.k_max + 1 : nmax), 16));
     const ws_plan wp = plan_workspace(m, T, n_work, QT);
     if (wp.total > workspace_bytes) SLED_FAIL(SLED_EINVAL, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, wp.total);
 
     // metadata blob
-    const size_t n_meta = 3 * (size_t)B + 2 * ((size_t)B + 1) + 2 * (size_t)T + (size_t)total_pages + work.size() + cu_work.size();
+    const size_t n_meta = 3 * (size_t)B + 2 * ((size_t)B + 1) + (tr ? 3 : 2) * (size_t)T + (size_t)total_pages + work.size() + cu_work.size();
     sled_stage_slot* sl;
     if ((rc = stage_acquire(p, n_meta, &sl)) != SLED_OK) return rc;
     int32_t* hp = sl->host;
     size_t o_req = 0, o_k = o_req + B, o_p0 = o_k + B, o_cur = o_p0 + B, o_cup = o_cur + B + 1, o_rr = o_cup + B + 1,
-           o_rj = o_rr + T, o_pg = o_rj + T, o_wk = o_pg + total_pages, o_cw = o_wk + work.size();
+           o_rj = o_rr + T, o_pg = o_rj + T, o_wk = o_pg + total_pages, o_cw = o_wk + work.size(), o_dp = o_cw + cu_work.size();
     int row = 0, pg = 0;
     for (int i = 0; i < B; i++) {
         const sled_request& rq = p->reqs[ent[i].req];
@@ -887,6 +916,7 @@ int run_forward(sled_model* m, sled_kvpool* p, const std::vector<step_entry>& en
     hp[o_cup + B] = pg;
     memcpy(hp + o_wk, work.data(), work.size() * sizeof(int32_t));
     memcpy(hp + o_cw, cu_work.data(), cu_work.size() * sizeof(int32_t));
+    if (tr) memcpy(hp + o_dp, tr->depth, T * sizeof(int32_t));
     SLED_HIP(hipMemcpyAsync(sl->dev, hp, n_meta * sizeof(int32_t), hipMemcpyHostToDevice, st));
     sled_step_meta meta;
     meta.req_id = sl->dev + o_req;
@@ -896,6 +926,7 @@ int run_forward(sled_model* m, sled_kvpool* p, const std::vector<step_entry>& en
     meta.cu_pages = sl->dev + o_cup;
     meta.row_req = sl->dev + o_rr;
     meta.row_j = sl->dev + o_rj;
+    meta.row_depth = sl->dev + (tr ? o_dp : o_rj);
     meta.pages = sl->dev + o_pg;
     meta.work = sl->dev + o_wk;
     meta.cu_work = sl->dev + o_cw;
@@ -937,7 +968,7 @@ int run_forward(sled_model* m, sled_kvpool* p, const std::vector<step_entry>& en
     // every block is a request of its own at offset 0, i.e. in a verification step.  The blocks of a prompt slice read
     // keys that other blocks of the same slice write, so there all new K/V must be in the cache before attention
     // starts: the stand-alone row kernel does it.
-    bool qkv_fused = bf;
+    bool qkv_fused = bf && !tr;
     for (const step_entry& e : ent) qkv_fused = qkv_fused && e.pos0 == 0;
     if (qkv_fused) {
         std::vector<char> seen(p->max_requests, 0);
@@ -962,7 +993,12 @@ int run_forward(sled_model* m, sled_kvpool* p, const std::vector<step_entry>& en
     for (int l = 0; l < s.n_layers; l++) {
         const sled_layer_weights& w = m->layers[l];
         SLED_RUN(SLED_PROF_PROJ, sled_launch_gemm(m, xa, pl_d, w.w_qkv, w.s_qkv, T, T_pad, m->n_qkv, d, SLED_EPI_PARTIAL, g_qkv, partial, nullptr, 0, 0, st));
-        if (qkv_fused) {
+        if (tr) {
+            const int KD = Hkv * s.head_dim;
+            SLED_RUN(SLED_PROF_ROWS, sled_launch_tree_qkv(m, T, partial, g_qkv.split, T_pad, cs, qb, pl_hd, tr->k, tr->v, st));
+            SLED_RUN(SLED_PROF_ATTN, sled_launch_tree_attention(m, p, *tr->plan, l, qb, HD, pl_hd, tr->k, KD, tr->v, KD, xo, pl_hd, tr->lse, true, st));
+            if (tr->mass) SLED_RUN(SLED_PROF_ATTN, sled_launch_tree_mass(m, p, *tr->plan, l, qb, HD, pl_hd, tr->lse, tr->mass, tr->cap, st));
+        } else if (qkv_fused) {
             SLED_RUN(SLED_PROF_ATTN, sled_launch_attention(m, p, meta, l, nullptr, 0, partial, g_qkv.split, T_pad, cs, kvslot, plan, part_o, part_ml, arrive, xo, pl_hd, QT, st));
         } else {
             SLED_RUN(SLED_PROF_ROWS, sled_launch_qkv_rope_store(m, p, T, l, partial, g_qkv.split, T_pad, cs, kvslot, qb, pl_hd, st));
@@ -1017,7 +1053,10 @@ extern "C" int sled_verify_batch(sled_model* m, sled_kvpool* p, int B, const int
     // what an earlier verify staged for requests that are not in this batch stays staged, but only the last batch
     // can be committed
     for (int r : p->last_batch) p->reqs[r].staged = -1;
-    for (int i = 0; i < B; i++) p->reqs[req_ids[i]].staged = k[i] + 1;
+    for (int i = 0; i < B; i++) {
+        leave_tree(p, req_ids[i]);
+        p->reqs[req_ids[i]].staged = k[i] + 1;
+    }
     p->last_batch.assign(req_ids, req_ids + B);
     return SLED_OK;
 }
@@ -1114,6 +1153,7 @@ extern "C" int sled_prefill(sled_model* m, sled_kvpool* p, int req_id, int n_tok
     // rows staged for THIS request by an earlier verify are overwritten, so it has nothing left to commit; the other
     // requests of that verify keep their staged rows and their commit stays valid
     rq.staged = -1;
+    leave_tree(p, req_id);
     for (int done = 0; done < n_tokens;) {
         const int rows = std::min(n_tokens - done, blocks_per_step * per);
         std::vector<step_entry> ent;
@@ -1128,7 +1168,7 @@ extern "C" int sled_prefill(sled_model* m, sled_kvpool* p, int req_id, int n_tok
         sl->host[0] = req_id;
         sl->host[1] = rows;
         SLED_HIP(hipMemcpyAsync(sl->dev, sl->host, 2 * sizeof(int32_t), hipMemcpyHostToDevice, st));
-        if ((rc = sled_launch_len_add(p->len_dev, sl->dev, sl->dev + 1, nullptr, nullptr, 1, st)) != SLED_OK) return rc;
+        if ((rc = sled_launch_len_add(p->len_dev, p->shift_dev, sl->dev, sl->dev + 1, nullptr, nullptr, 1, st)) != SLED_OK) return rc;
         if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
         rq.len_ub += rows;
         rq.added += rows;
@@ -1211,3 +1251,491 @@ extern "C" int sled_row_confidence(int T, int vocab, float temperature, const fl
     if (need > workspace_bytes) SLED_FAIL(SLED_EINVAL, "sled_row_confidence: workspace of %zu bytes, %zu needed", workspace_bytes, need);
     return sled_launch_row_confidence(T, vocab, temperature, logits, conf, top, workspace, static_cast<hipStream_t>(stream));
 }
+
+// ------------------------------------------------------------------------------------------ trees
+// The host side's own allocations may fail; nothing is thrown over the C boundary.
+#define SLED_CATCH(who)                                                        \
+    catch (const std::exception& e) {                                          \
+        sled_set_error("%s: host allocation failed (%s)", who, e.what());      \
+        return SLED_ENOMEM;                                                    \
+    }
+
+namespace {
+
+// Calls that send metadata from a staging buffer cannot be replayed: the buffer holds another call's by then.
+int refuse_capture(hipStream_t st, const char* who) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    SLED_HIP(hipStreamIsCapturing(st, &status));
+    if (status != hipStreamCaptureStatusNone) SLED_FAIL(SLED_ESTATE, "%s cannot be captured into a graph", who);
+    return SLED_OK;
+}
+
+constexpr int MASS_ITEM_PAGES = 32;   // of a workgroup of the mass kernel: four for each of its eight wavefronts
+
+// a plan in the caller's workspace
+struct tree_layout {
+    size_t mass_items, seen, pages, arrive, ints, part_o, part_ml, total;   // byte offsets; the first `ints` bytes come from the host
+};
+tree_layout tree_plan_layout(const sled_model* m, int64_t n_items, int64_t n_mass, int T, int64_t n_pages, int tiles) {
+    tree_layout w;
+    size_t off = align_up((size_t)n_items * SLED_TREE_ITEM * 4, 16);
+    w.mass_items = off;
+    off += align_up((size_t)n_mass * 8 * 4, 16);
+    w.seen = off;
+    off += align_up((size_t)T * 8, 16);
+    w.pages = off;
+    off += align_up((size_t)n_pages * 4, 16);
+    w.arrive = off;
+    off += (size_t)n_items * 4 * 4;
+    w.ints = off;
+    off = align_up(off, 256);
+    w.part_o = off;
+    off += align_up((size_t)n_items * tiles * 16 * m->s.head_dim * sizeof(float), 256);
+    w.part_ml = off;
+    off += align_up((size_t)n_items * 2 * tiles * 16 * sizeof(float), 256);
+    w.total = off;
+    return w;
+}
+
+size_t tree_plan_bytes(const sled_model* m, int B, int T, int64_t ctx_tokens) {
+    const int Hkv = m->s.n_kv_heads, G = m->s.n_q_heads / Hkv;
+    const int64_t n_pages = ctx_tokens / 16 + 2 * (int64_t)B, n_mass = Hkv * (n_pages / MASS_ITEM_PAGES + B);
+    size_t worst = 0;
+    for (int tiles = 1; tiles <= SLED_TREE_TILES; tiles *= 2) {
+        // (request, row group) pairs: several groups only where the most tiles do not hold a request's rows
+        constexpr int GROUP = 16 * SLED_TREE_TILES;
+        const int64_t groups = tiles < SLED_TREE_TILES ? B : std::min<int64_t>((int64_t)B * ceil_div(SLED_TREE_MAX * G, GROUP), B + (int64_t)T * G / GROUP);
+        int64_t items = attn_item_cap((int)groups, Hkv) + groups * Hkv;
+        if (m->batch_invariant) items = std::max(items, (ctx_tokens / (16 * SLED_FIXED_CHUNK_PAGES) + B) * Hkv * ceil_div((int)groups, B));
+        worst = std::max(worst, tree_plan_layout(m, items, n_mass, T, n_pages, tiles).total);
+    }
+    return worst;
+}
+
+int check_trees(int B, const int* n_nodes, const int* parent, int* T_out, int* depth_out, std::vector<int>* depths, const char* who) {
+    int64_t T = 0;
+    int deepest = 0;
+    for (int i = 0; i < B; i++) {
+        if (n_nodes[i] < 1 || n_nodes[i] > SLED_TREE_MAX) SLED_FAIL(SLED_EINVAL, "%s: tree %d has %d nodes, outside [1, %d]", who, i, n_nodes[i], SLED_TREE_MAX);
+        int d[SLED_TREE_MAX];
+        d[0] = 0;
+        for (int j = 1; j < n_nodes[i]; j++) {
+            const int q = parent[T + j];
+            if (q < 0 || q >= j) SLED_FAIL(SLED_EINVAL, "%s: tree %d: node %d continues node %d, which does not come before it", who, i, j, q);
+            d[j] = d[q] + 1;
+            deepest = std::max(deepest, d[j]);
+        }
+        if (depths) depths->insert(depths->end(), d, d + n_nodes[i]);
+        T += n_nodes[i];
+    }
+    *T_out = (int)T;
+    if (depth_out) *depth_out = deepest;
+    return SLED_OK;
+}
+
+// Pages of a work item of the tree attention: every (request, kv head, row group) splits its context evenly into items of at most so many.
+// A launch of no more items than CUs takes as long as its longest; a longer one about its share of the whole on each CU and some of an item
+// more.  An item's own start and end count as ITEM_FIXED pages and, where its context is split, ITEM_SPLIT more.
+int tree_pages_per_item(const std::vector<int>& np, const std::vector<int>& groups, int Hkv) {
+    constexpr int ITEM_FIXED = 24, ITEM_SPLIT = 12, LEAST = 16;
+    int longest = 1;
+    for (int n : np) longest = std::max(longest, n);
+    int best = longest;
+    double best_end = -1.0;
+    for (int pieces = 1; pieces <= 64; pieces += std::max(1, pieces / 4)) {
+        const int tgt = ceil_div(longest, pieces);
+        if (pieces > 1 && tgt < LEAST) break;
+        int64_t items = 0, total = 0;
+        for (size_t i = 0; i < np.size(); i++) {
+            const int64_t n = std::max(1, ceil_div(np[i], tgt)), mult = (int64_t)groups[i] * Hkv;
+            items += mult * n;
+            total += mult * (np[i] + n * (ITEM_FIXED + (n > 1 ? ITEM_SPLIT : 0)));
+        }
+        int64_t pairs = 0;
+        for (int g : groups) pairs += (int64_t)g;
+        if (items > attn_item_cap((int)pairs, Hkv)) break;
+        const double one = tgt + ITEM_FIXED + (pieces > 1 ? ITEM_SPLIT : 0), share = (double)total / ATTN_CUS;
+        const double end = items <= ATTN_CUS ? one : std::max(one, share) + 0.5 * total / items;
+        if (best_end < 0 || end < best_end) {
+            best_end = end;
+            best = tgt;
+        }
+    }
+    return best;
+}
+
+// The plan of a batch of trees: pages for their nodes, which nodes each sees, work items.  p->tree is valid afterwards.
+int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, const int* parent, void* workspace, size_t workspace_bytes, hipStream_t st,
+               const char* who) {
+    const sled_model* m = p->m;
+    const int Hkv = m->s.n_kv_heads, G = m->s.n_q_heads / Hkv, P = m->s.dtype == SLED_BF16 ? 2 : 1;
+    int rc, T = 0, nmax = 0, reach_max = 0;
+    int64_t n_pages = 0;
+    std::vector<int> np(B);   // context pages
+    for (int i = 0; i < B; i++) {
+        const sled_request& rq = p->reqs[req_ids[i]];
+        if ((rc = ensure_pages(p, req_ids[i], rq.len_ub + n_nodes[i])) != SLED_OK) return rc;
+        np[i] = ceil_div(rq.len_ub, 16);
+        n_pages += ceil_div(rq.len_ub + n_nodes[i], 16);
+        reach_max = std::max(reach_max, rq.len_ub + n_nodes[i]);
+        nmax = std::max(nmax, n_nodes[i]);
+        T += n_nodes[i];
+    }
+    int tiles = 1;
+    while (tiles < SLED_TREE_TILES && 16 * tiles < G * nmax) tiles *= 2;
+    std::vector<int> groups(B);
+    for (int i = 0; i < B; i++) groups[i] = ceil_div(G * n_nodes[i], 16 * tiles);
+    const int tgt = m->batch_invariant ? SLED_FIXED_CHUNK_PAGES : tree_pages_per_item(np, groups, Hkv);
+    auto chunk_of = [&](int i) {
+        const int c = m->batch_invariant ? SLED_FIXED_CHUNK_PAGES : attn_chunk(std::max(np[i], 1), tgt);
+        return ceil_div(c, P) * P;   // a step of the kernel is P pages
+    };
+    int64_t n_items = 0, n_mass = 0, mass_chunk = MASS_ITEM_PAGES;
+    while (n_pages * Hkv / mass_chunk > 8192) mass_chunk *= 2;
+    for (int i = 0; i < B; i++) {
+        n_items += (int64_t)groups[i] * Hkv * std::max(1, ceil_div(np[i], chunk_of(i)));
+        n_mass += (int64_t)Hkv * ceil_div(ceil_div(p->reqs[req_ids[i]].len_ub + n_nodes[i], 16), (int)mass_chunk);
+    }
+    const tree_layout w = tree_plan_layout(m, n_items, n_mass, T, n_pages, tiles);
+    if (w.total > workspace_bytes) SLED_FAIL(SLED_EINVAL, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, w.total);
+    sled_stage_slot* sl;
+    if ((rc = stage_acquire(p, w.ints / 4, &sl)) != SLED_OK) return rc;
+    char* host = reinterpret_cast<char*>(sl->host);
+    int32_t *item = sl->host, *mass_item = reinterpret_cast<int32_t*>(host + w.mass_items), *pages = reinterpret_cast<int32_t*>(host + w.pages);
+    uint64_t* seen = reinterpret_cast<uint64_t*>(host + w.seen);
+    memset(host + w.arrive, 0, w.ints - w.arrive);
+    // longest contexts first, so that little is left for the end of the launch (batch-invariant: nothing may depend on the other requests, and
+    // no result does on the order)
+    std::vector<int> by_length(B), row0(B), page_at(B);
+    int row = 0, pg = 0;
+    for (int i = 0; i < B; i++) {
+        by_length[i] = i;
+        row0[i] = row;
+        page_at[i] = pg;
+        for (int j = 0; j < n_nodes[i]; j++) seen[row + j] = (uint64_t)1 << j | (j ? seen[row + parent[row + j]] : 0);
+        const sled_request& rq = p->reqs[req_ids[i]];
+        const int mine = ceil_div(rq.len_ub + n_nodes[i], 16);
+        for (int q = 0; q < mine; q++) pages[pg + q] = rq.pages[q];
+        pg += mine;
+        row += n_nodes[i];
+    }
+    std::stable_sort(by_length.begin(), by_length.end(), [&](int a, int b) { return np[a] > np[b]; });
+    int at = 0;
+    for (int i : by_length) {
+        const int chunk = chunk_of(i), runs = std::max(1, ceil_div(np[i], chunk)), first = at, stride = groups[i] * Hkv;
+        for (int c = 0; c < runs; c++)
+            for (int r = 0; r < groups[i]; r++)
+                for (int g = 0; g < Hkv; g++, at++) {
+                    const int32_t rec[SLED_TREE_ITEM] = {req_ids[i], g, c * chunk, std::min(chunk, np[i] - c * chunk), n_nodes[i], row0[i], page_at[i],
+                                                         first + r * Hkv + g, runs, stride, r * 16 * tiles, c == runs - 1};
+                    memcpy(item + (size_t)at * SLED_TREE_ITEM, rec, sizeof(rec));
+                }
+        const int all = ceil_div(p->reqs[req_ids[i]].len_ub + n_nodes[i], 16);
+        for (int p0 = 0; p0 < all; p0 += (int)mass_chunk)
+            for (int g = 0; g < Hkv; g++, mass_item += 8) {
+                const int32_t rec[8] = {req_ids[i], g, p0, std::min((int)mass_chunk, all - p0), n_nodes[i], row0[i], page_at[i], 0};
+                memcpy(mass_item, rec, sizeof(rec));
+            }
+    }
+    SLED_HIP(hipMemcpyAsync(workspace, sl->host, w.ints, hipMemcpyHostToDevice, st));
+    if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
+    char* ws = static_cast<char*>(workspace);
+    sled_tree_plan& t = p->tree.plan;
+    t.items = reinterpret_cast<const int32_t*>(ws);
+    t.mass_items = reinterpret_cast<const int32_t*>(ws + w.mass_items);
+    t.seen = reinterpret_cast<const uint64_t*>(ws + w.seen);
+    t.pages = reinterpret_cast<const int32_t*>(ws + w.pages);
+    t.arrive = reinterpret_cast<int32_t*>(ws + w.arrive);
+    t.part_o = reinterpret_cast<float*>(ws + w.part_o);
+    t.part_ml = reinterpret_cast<float*>(ws + w.part_ml);
+    t.n_items = (int)n_items;
+    t.n_mass_items = (int)n_mass;
+    t.tiles = tiles;
+    t.max_nodes = nmax;
+    t.T = T;
+    // what earlier steps staged for these requests is overwritten, and only the last trees can be committed
+    for (int r : p->tree.reqs) p->reqs[r].staged = -1;
+    for (int i = 0; i < B; i++) {
+        p->last_batch.erase(std::remove(p->last_batch.begin(), p->last_batch.end(), req_ids[i]), p->last_batch.end());
+        p->reqs[req_ids[i]].staged = n_nodes[i];
+    }
+    p->tree.reqs.assign(req_ids, req_ids + B);
+    p->tree.workspace = workspace;
+    p->tree.max_reach = reach_max;
+    p->tree.valid = true;
+    return SLED_OK;
+}
+
+// checks shared by the calls that open a step over trees
+int begin_checks(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, const int* parent, const void* workspace, hipStream_t st, int* T,
+                 std::vector<int>* depths, const char* who) {
+    if (!p || !req_ids || !n_nodes || !parent || !workspace) SLED_FAIL(SLED_EINVAL, "%s: null argument", who);
+    if (reinterpret_cast<uintptr_t>(workspace) % 256) SLED_FAIL(SLED_EINVAL, "%s: workspace must be 256-byte aligned", who);
+    int rc = check_requests(p, B, req_ids, who);
+    if (rc != SLED_OK) return rc;
+    if ((rc = check_trees(B, n_nodes, parent, T, nullptr, depths, who)) != SLED_OK) return rc;
+    return refuse_capture(st, who);
+}
+
+int check_mass(const sled_kvpool* p, int mass_cap, int reach, const char* who) {
+    if (mass_cap < reach)
+        SLED_FAIL(SLED_EINVAL, "%s: mass rows of %d entries, but a request may reach %d tokens (sled_kvpool_lengths gives exact lengths to the library)", who,
+                  mass_cap, reach);
+    (void)p;
+    return SLED_OK;
+}
+
+// rows of `width` elements, `stride` apart
+int check_rows(const sled_model* m, const void* x, int64_t stride, int width, const char* what, const char* who) {
+    if (!x) SLED_FAIL(SLED_EINVAL, "%s: null %s", who, what);
+    if (reinterpret_cast<uintptr_t>(x) % 16 || stride < width || stride * (int64_t)m->elem % 16)
+        SLED_FAIL(SLED_EINVAL, "%s: rows of %s must be 16-byte aligned and at least %d elements apart", who, what, width);
+    return SLED_OK;
+}
+
+struct verify_tree_layout {
+    size_t k, v, lse, plan, total;
+};
+verify_tree_layout lay_out_verify_tree(const sled_model* m, int T) {
+    const ws_plan wp = plan_workspace(m, T, 0, 1);
+    const size_t kv = align_up((size_t)T * m->s.n_kv_heads * m->s.head_dim * m->elem, 256);
+    verify_tree_layout w;
+    w.k = align_up(wp.total, 256);
+    w.v = w.k + kv;
+    w.lse = w.v + kv;
+    w.plan = w.lse + align_up((size_t)T * m->s.n_q_heads * sizeof(float), 256);
+    w.total = w.plan;
+    return w;
+}
+
+}  // namespace
+
+extern "C" size_t sled_tree_workspace_bytes(const sled_model* m, int B_max, int T_max, int64_t ctx_tokens_max) {
+    if (!m || B_max < 1 || T_max < 1 || ctx_tokens_max < 0) return 0;
+    return tree_plan_bytes(m, B_max, T_max, ctx_tokens_max);
+}
+
+extern "C" int sled_tree_begin(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, const int* parent, void* workspace, size_t workspace_bytes,
+                               void* stream) try {
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    int T;
+    int rc = begin_checks(p, B, req_ids, n_nodes, parent, workspace, st, &T, nullptr, "sled_tree_begin");
+    if (rc != SLED_OK) return rc;
+    poll_readbacks(p);
+    if ((rc = reset_fresh_lengths(p, B, req_ids, st)) != SLED_OK) return rc;
+    return plan_trees(p, B, req_ids, n_nodes, parent, workspace, workspace_bytes, st, "sled_tree_begin");
+}
+SLED_CATCH("sled_tree_begin")
+
+extern "C" int sled_tree_attention(sled_kvpool* p, int layer, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                   void* out, float* lse, void* workspace, void* stream) {
+    if (!p) SLED_FAIL(SLED_EINVAL, "sled_tree_attention: null pool");
+    if (!p->tree.valid) SLED_FAIL(SLED_ESTATE, "sled_tree_attention: no trees at hand (sled_tree_begin comes first)");
+    const sled_model* m = p->m;
+    if (layer < 0 || layer >= m->s.n_layers) SLED_FAIL(SLED_EINVAL, "sled_tree_attention: layer %d out of range", layer);
+    if (workspace != p->tree.workspace) SLED_FAIL(SLED_EINVAL, "sled_tree_attention: not the workspace that sled_tree_begin was given");
+    const int HD = m->s.n_q_heads * m->s.head_dim, KD = m->s.n_kv_heads * m->s.head_dim;
+    int rc;
+    if ((rc = check_rows(m, q, q_stride, HD, "q", "sled_tree_attention")) != SLED_OK || (rc = check_rows(m, k, k_stride, KD, "k", "sled_tree_attention")) != SLED_OK ||
+        (rc = check_rows(m, v, v_stride, KD, "v", "sled_tree_attention")) != SLED_OK || (rc = check_rows(m, out, HD, HD, "out", "sled_tree_attention")) != SLED_OK)
+        return rc;
+    return sled_launch_tree_attention(m, p, p->tree.plan, layer, q, q_stride, 0, k, k_stride, v, v_stride, out, 0, lse, false, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int sled_tree_mass(sled_kvpool* p, int layer, const void* q, int64_t q_stride, const float* lse, float* mass, int mass_cap, void* workspace, void* stream) {
+    if (!p || !lse || !mass) SLED_FAIL(SLED_EINVAL, "sled_tree_mass: null argument");
+    if (!p->tree.valid) SLED_FAIL(SLED_ESTATE, "sled_tree_mass: no trees at hand (sled_tree_begin comes first)");
+    const sled_model* m = p->m;
+    if (layer < 0 || layer >= m->s.n_layers) SLED_FAIL(SLED_EINVAL, "sled_tree_mass: layer %d out of range", layer);
+    if (workspace != p->tree.workspace) SLED_FAIL(SLED_EINVAL, "sled_tree_mass: not the workspace that sled_tree_begin was given");
+    int rc;
+    if ((rc = check_rows(m, q, q_stride, m->s.n_q_heads * m->s.head_dim, "q", "sled_tree_mass")) != SLED_OK) return rc;
+    if ((rc = check_mass(p, mass_cap, p->tree.max_reach, "sled_tree_mass")) != SLED_OK) return rc;
+    return sled_launch_tree_mass(m, p, p->tree.plan, layer, q, q_stride, 0, lse, mass, mass_cap, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int sled_tree_commit(sled_kvpool* p, int B, const int* req_ids, const int32_t* accept_len, const int32_t* path, float* mass, int mass_cap, void* stream) try {
+    if (!p || !req_ids || !accept_len || !path) SLED_FAIL(SLED_EINVAL, "sled_tree_commit: null argument");
+    int rc = check_requests(p, B, req_ids, "sled_tree_commit");
+    if (rc != SLED_OK) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if ((rc = refuse_capture(st, "sled_tree_commit")) != SLED_OK) return rc;
+    poll_readbacks(p);
+    size_t need = 3 * (size_t)B;
+    for (int i = 0; i < B; i++) {
+        const sled_request& rq = p->reqs[req_ids[i]];
+        if (std::find(p->tree.reqs.begin(), p->tree.reqs.end(), req_ids[i]) == p->tree.reqs.end() || rq.staged < 0)
+            SLED_FAIL(SLED_ESTATE, "sled_tree_commit: request %d has no tree staged", req_ids[i]);
+        if (mass && (rc = check_mass(p, mass_cap, rq.len_ub + rq.staged, "sled_tree_commit")) != SLED_OK) return rc;
+        need += rq.pages.size();
+    }
+    sled_stage_slot* sl;
+    if ((rc = stage_acquire(p, need, &sl)) != SLED_OK) return rc;
+    size_t off = 3 * (size_t)B;
+    for (int i = 0; i < B; i++) {
+        const sled_request& rq = p->reqs[req_ids[i]];
+        sl->host[3 * i] = req_ids[i];
+        sl->host[3 * i + 1] = rq.staged;
+        sl->host[3 * i + 2] = (int32_t)(off - 3 * (size_t)B);
+        for (int pg : rq.pages) sl->host[off++] = pg;
+    }
+    SLED_HIP(hipMemcpyAsync(sl->dev, sl->host, off * sizeof(int32_t), hipMemcpyHostToDevice, st));
+    if ((rc = sled_launch_tree_commit(p->m, p, sl->dev, sl->dev + 3 * B, B, accept_len, path, mass, mass_cap, st)) != SLED_OK) return rc;
+    if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
+    for (int i = 0; i < B; i++) {
+        sled_request& rq = p->reqs[req_ids[i]];
+        rq.len_ub += rq.staged;   // every node of a chain may have been accepted; the exact lengths follow
+        rq.added += rq.staged;
+        rq.staged = -1;
+        leave_tree(p, req_ids[i]);
+    }
+    return enqueue_readback(p, B, req_ids, st);
+}
+SLED_CATCH("sled_tree_commit")
+
+extern "C" size_t sled_verify_tree_workspace_bytes(const sled_model* m, int B_max, int T_max, int64_t ctx_tokens_max) {
+    if (!m || B_max < 1 || T_max < 1 || ctx_tokens_max < 0) return 0;
+    return lay_out_verify_tree(m, T_max).total + tree_plan_bytes(m, B_max, T_max, ctx_tokens_max);
+}
+
+extern "C" int sled_verify_tree(sled_model* m, sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, const int* parent, const int32_t* tokens, float* logits,
+                                float* mass, int mass_cap, void* workspace, size_t workspace_bytes, void* stream) try {
+    if (!m || !tokens || !logits) SLED_FAIL(SLED_EINVAL, "sled_verify_tree: null argument");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    int T;
+    std::vector<int> depth;
+    int rc = begin_checks(p, B, req_ids, n_nodes, parent, workspace, st, &T, &depth, "sled_verify_tree");
+    if (rc != SLED_OK) return rc;
+    if (p->m != m) SLED_FAIL(SLED_EINVAL, "sled_verify_tree: pool belongs to another model");
+    poll_readbacks(p);
+    for (int i = 0; mass && i < B; i++)
+        if ((rc = check_mass(p, mass_cap, p->reqs[req_ids[i]].len_ub + n_nodes[i], "sled_verify_tree")) != SLED_OK) return rc;
+    if ((rc = reset_fresh_lengths(p, B, req_ids, st)) != SLED_OK) return rc;
+    const verify_tree_layout w = lay_out_verify_tree(m, T);
+    if (w.plan > workspace_bytes) SLED_FAIL(SLED_EINVAL, "sled_verify_tree: workspace of %zu bytes, more than %zu needed", workspace_bytes, w.plan);
+    char* ws = static_cast<char*>(workspace);
+    if ((rc = plan_trees(p, B, req_ids, n_nodes, parent, ws + w.plan, workspace_bytes - w.plan, st, "sled_verify_tree")) != SLED_OK) return rc;
+    p->tree.valid = false;   // (the plan serves this step alone; the nodes stay staged for the commit)
+    std::vector<step_entry> ent(B);
+    for (int i = 0; i < B; i++) ent[i] = step_entry{req_ids[i], 0, n_nodes[i]};
+    const tree_step tr{&p->tree.plan, depth.data(), ws + w.k, ws + w.v, reinterpret_cast<float*>(ws + w.lse), mass, mass_cap};
+    return run_forward(m, p, ent, tokens, logits, -1, nullptr, workspace, w.k, st, "sled_verify_tree", &tr);
+}
+SLED_CATCH("sled_verify_tree")
+
+extern "C" size_t sled_accept_tree_workspace_bytes(int B, int T, int vocab) {
+    if (B < 1 || T < 1 || vocab < 2) return 0;
+    return sled_accept_tree_ws_bytes(B, T, vocab);
+}
+
+extern "C" int sled_accept_tree(int mode, int B, const int* n_nodes, const int* parent, int vocab, float temperature, const float* logits, const int32_t* tokens,
+                                const float* u, int32_t* accept_len, int32_t* path, int32_t* out_token, void* workspace, size_t workspace_bytes, void* stream) try {
+    if (!n_nodes || !parent || !logits || !tokens || !accept_len || !path || !out_token || !workspace) SLED_FAIL(SLED_EINVAL, "sled_accept_tree: null argument");
+    if (mode != SLED_GREEDY && mode != SLED_SAMPLE) SLED_FAIL(SLED_EINVAL, "sled_accept_tree: unknown mode %d", mode);
+    if (mode == SLED_SAMPLE && !u) SLED_FAIL(SLED_EINVAL, "sled_accept_tree: sampling needs u");
+    if (B < 1 || B > 1024) SLED_FAIL(SLED_EINVAL, "sled_accept_tree: batch size %d outside [1, 1024]", B);
+    if (vocab < 2 || vocab > 2000000) SLED_FAIL(SLED_EINVAL, "sled_accept_tree: vocab %d unsupported", vocab);
+    if (!(temperature > 0.f)) SLED_FAIL(SLED_EINVAL, "sled_accept_tree: temperature must be positive");
+    int T, depth;
+    int rc = check_trees(B, n_nodes, parent, &T, &depth, nullptr, "sled_accept_tree");
+    if (rc != SLED_OK) return rc;
+    if (reinterpret_cast<uintptr_t>(workspace) % 256) SLED_FAIL(SLED_EINVAL, "sled_accept_tree: workspace must be 256-byte aligned");
+    const size_t need = sled_accept_tree_ws_bytes(B, T, vocab);
+    if (need > workspace_bytes) SLED_FAIL(SLED_EINVAL, "sled_accept_tree: workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    return sled_launch_accept_tree(mode, B, T, n_nodes, parent, depth, vocab, temperature, logits, tokens, u, accept_len, path, out_token, workspace,
+                                   static_cast<hipStream_t>(stream));
+}
+SLED_CATCH("sled_accept_tree")
+
+// ------------------------------------------------------------------------------------------ eviction
+extern "C" size_t sled_kv_evict_workspace_bytes(const sled_model* m, int B_max, int keep_max) {
+    if (!m || B_max < 1 || keep_max < 1) return 0;
+    return align_up((size_t)B_max * m->s.n_layers * m->s.n_kv_heads * keep_max * sizeof(int32_t), 256);
+}
+
+extern "C" int sled_kv_evict(sled_kvpool* p, int B, const int* req_ids, const int* dst_ids, const int* keep, int n_first, int n_recent, float* mass, int mass_cap,
+                             void* workspace, size_t workspace_bytes, void* stream) try {
+    if (!p || !req_ids || !keep || !mass || !workspace) SLED_FAIL(SLED_EINVAL, "sled_kv_evict: null argument");
+    if (reinterpret_cast<uintptr_t>(workspace) % 256) SLED_FAIL(SLED_EINVAL, "sled_kv_evict: workspace must be 256-byte aligned");
+    int rc = check_requests(p, B, req_ids, "sled_kv_evict");
+    if (rc != SLED_OK) return rc;
+    if (n_first < 0 || n_recent < 0) SLED_FAIL(SLED_EINVAL, "sled_kv_evict: negative n_first or n_recent");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if ((rc = refuse_capture(st, "sled_kv_evict")) != SLED_OK) return rc;
+    const bool in_place = !dst_ids;
+    poll_readbacks(p);
+    if (!in_place) {
+        if ((rc = check_requests(p, B, dst_ids, "sled_kv_evict")) != SLED_OK) return rc;
+        for (int i = 0; i < B; i++) {
+            if (std::find(req_ids, req_ids + B, dst_ids[i]) != req_ids + B) SLED_FAIL(SLED_EINVAL, "sled_kv_evict: request %d is source and destination", dst_ids[i]);
+            if (p->reqs[dst_ids[i]].len_ub > 0 || p->reqs[dst_ids[i]].staged >= 0)
+                SLED_FAIL(SLED_ESTATE, "sled_kv_evict: destination request %d is not empty", dst_ids[i]);
+        }
+    }
+    int keep_max = 0;
+    for (int i = 0; i < B; i++) {
+        if (keep[i] < 1 || (int64_t)n_first + n_recent > keep[i])
+            SLED_FAIL(SLED_EINVAL, "sled_kv_evict: keep[%d] = %d, at least 1 and n_first + n_recent = %lld needed", i, keep[i], (long long)n_first + n_recent);
+        if ((rc = check_mass(p, mass_cap, p->reqs[req_ids[i]].len_ub, "sled_kv_evict")) != SLED_OK) return rc;
+        keep_max = std::max(keep_max, std::min(keep[i], p->reqs[req_ids[i]].len_ub));
+    }
+    const size_t idx_bytes = (size_t)B * p->m->s.n_layers * p->m->s.n_kv_heads * keep_max * sizeof(int32_t);
+    if (idx_bytes > workspace_bytes) SLED_FAIL(SLED_EINVAL, "sled_kv_evict: workspace of %zu bytes, %zu needed", workspace_bytes, idx_bytes);
+    if ((rc = reset_fresh_lengths(p, B, req_ids, st)) != SLED_OK) return rc;
+    if (!in_place && (rc = reset_fresh_lengths(p, B, dst_ids, st)) != SLED_OK) return rc;
+    size_t need = (size_t)SLED_EVICT_REC * B;
+    for (int i = 0; i < B; i++) {
+        const int src_ub = p->reqs[req_ids[i]].len_ub;
+        if (!in_place && (rc = ensure_pages(p, dst_ids[i], std::min(keep[i], src_ub))) != SLED_OK) return rc;
+        need += p->reqs[req_ids[i]].pages.size() + (in_place ? 0 : p->reqs[dst_ids[i]].pages.size());
+    }
+    sled_stage_slot* sl;
+    if ((rc = stage_acquire(p, need, &sl)) != SLED_OK) return rc;
+    int32_t* pages = sl->host + (size_t)SLED_EVICT_REC * B;
+    int pg = 0;
+    for (int i = 0; i < B; i++) {
+        int32_t* rec = sl->host + (size_t)SLED_EVICT_REC * i;
+        rec[0] = req_ids[i];
+        rec[1] = in_place ? req_ids[i] : dst_ids[i];
+        rec[2] = keep[i];
+        rec[3] = rec[4] = pg;
+        for (int q : p->reqs[req_ids[i]].pages) pages[pg++] = q;
+        if (!in_place) {
+            rec[4] = pg;
+            for (int q : p->reqs[dst_ids[i]].pages) pages[pg++] = q;
+        }
+    }
+    SLED_HIP(hipMemcpyAsync(sl->dev, sl->host, need * sizeof(int32_t), hipMemcpyHostToDevice, st));
+    if (keep_max > 0 && (rc = sled_launch_evict(p->m, p, sl->dev, sl->dev + (size_t)SLED_EVICT_REC * B, B, keep_max, n_first, n_recent, mass, mass_cap,
+                                                static_cast<int32_t*>(workspace), keep_max, in_place, st)) != SLED_OK)
+        return rc;
+    if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
+    for (int i = 0; i < B; i++) {
+        sled_request& src = p->reqs[req_ids[i]];
+        const int ub = std::min(keep[i], src.len_ub);
+        if (in_place) {
+            src.staged = -1;   // the tail slots have moved: nothing is left to commit
+            leave_tree(p, req_ids[i]);
+            src.len_ub = ub;
+            trim_pages(p, src);   // whoever gets the pages next writes them behind the kernels that read them here
+        } else {
+            p->reqs[dst_ids[i]].len_ub = ub;
+            p->reqs[dst_ids[i]].added += ub;
+        }
+    }
+    return SLED_OK;
+}
+SLED_CATCH("sled_kv_evict")
+
+extern "C" int sled_kvpool_positions(sled_kvpool* p, int B, const int* req_ids, int* positions, void* stream) try {
+    if (!p || !req_ids || !positions) SLED_FAIL(SLED_EINVAL, "sled_kvpool_positions: null argument");
+    int rc = check_requests(p, B, req_ids, "sled_kvpool_positions");
+    if (rc != SLED_OK) return rc;
+    SLED_HIP(hipStreamSynchronize(static_cast<hipStream_t>(stream)));
+    std::vector<int32_t> len(p->max_requests), shift(p->max_requests);
+    SLED_HIP(hipMemcpy(len.data(), p->len_dev, len.size() * sizeof(int32_t), hipMemcpyDeviceToHost));
+    SLED_HIP(hipMemcpy(shift.data(), p->shift_dev, shift.size() * sizeof(int32_t), hipMemcpyDeviceToHost));
+    for (int i = 0; i < B; i++) positions[i] = p->reqs[req_ids[i]].fresh ? 0 : len[req_ids[i]] + shift[req_ids[i]];
+    return SLED_OK;
+}
+SLED_CATCH("sled_kvpool_positions")

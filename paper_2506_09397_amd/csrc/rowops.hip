@@ -195,7 +195,8 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const float* __rest
 
 // Everything a step needs before its first projection, in one launch (four of them one after the other took 16 us, 5 of which are a launch's
 // own time each; together they take as long as the longest, the rotary table's float64 functions):
-//   rotary table   per packed row cos/sin of pos * theta^(-2i/D), evaluated in float64 and stored as float32, and where the row's K/V go
+//   rotary table   per packed row cos/sin of pos * theta^(-2i/D), evaluated in float64 and stored as float32 (pos: the row's place in the text;
+//                  tokens that were evicted from the cache still count), and where the row's K/V go
 //                  (16 * page + slot) -- the chain of dependent lookups behind that is then paid once, not in every layer
 //   work records   (bf16 models) per attention work item everything its workgroup needs to know before it can request its first
 //                  page, gathered into one 48-byte record -- otherwise each of the step's attention launches starts with a chain of
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const float* __rest
 //                  first (the others follow Hkv places apart), how many
 //   embedding      h[t,:] = E[token]; X[t,:] = rmsnorm(h) * gain
 struct step_setup {
-    const int32_t* len_dev;
+    const int32_t *len_dev, *shift_dev;
     int half, Hkv;
     double theta;
     float2* cs;
@@ -228,8 +229,8 @@ __global__ __launch_bounds__(256) void step_setup_kernel(sled_step_meta meta, st
         const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
         if (t >= meta.T) return;
         const int b = meta.row_req[t];
-        const int pos = a.len_dev[meta.req_id[b]] + meta.pos0[b] + meta.row_j[t];
-        if (lane == 0) a.kvslot[t] = meta.pages[meta.cu_pages[b] + (pos >> 4)] * 16 + (pos & 15);
+        const int from = a.len_dev[meta.req_id[b]] + meta.pos0[b], slot = from + meta.row_j[t], pos = from + a.shift_dev[meta.req_id[b]] + meta.row_depth[t];
+        if (lane == 0) a.kvslot[t] = meta.pages[meta.cu_pages[b] + (slot >> 4)] * 16 + (slot & 15);
         for (int i = lane; i < a.half; i += 64) {
             double inv = pow(a.theta, -(double)i / (double)a.half);
             double ang = (double)pos * inv;
@@ -584,19 +585,20 @@ __global__ __launch_bounds__(256) void copy_act_row_kernel(const void* __restric
 }
 
 // committed lengths after an append (+ add[i]) or, with `accept`, a commit (+ accept[i] + 1); `fresh`: the request starts from zero whatever the slot held
-__global__ void len_add_kernel(int32_t* __restrict__ len_dev, const int32_t* __restrict__ req_ids, const int32_t* __restrict__ add,
-                               const int32_t* __restrict__ fresh, const int32_t* __restrict__ accept, int B) {
+__global__ void len_add_kernel(int32_t* __restrict__ len_dev, int32_t* __restrict__ shift_dev, const int32_t* __restrict__ req_ids,
+                               const int32_t* __restrict__ add, const int32_t* __restrict__ fresh, const int32_t* __restrict__ accept, int B) {
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
     if (i >= B) return;
     const int r = req_ids[i], from = fresh && fresh[i] ? 0 : len_dev[r];
+    if (fresh && fresh[i]) shift_dev[r] = 0;
     len_dev[r] = from + (accept ? accept[i] + 1 : add[i]);
 }
-// the lengths of requests that have just been opened, up to 128 in a launch
+// the lengths (and positions) of requests that have just been opened, up to 128 in a launch
 struct len_ids {
     int id[128];
 };
-__global__ void len_zero_kernel(int32_t* __restrict__ len_dev, len_ids ids, int n) {
-    if ((int)threadIdx.x < n) len_dev[ids.id[threadIdx.x]] = 0;
+__global__ void len_zero_kernel(int32_t* __restrict__ len_dev, int32_t* __restrict__ shift_dev, len_ids ids, int n) {
+    if ((int)threadIdx.x < n) len_dev[ids.id[threadIdx.x]] = shift_dev[ids.id[threadIdx.x]] = 0;
 }
 
 // ----- weight repacking --------------------------------------------------------------------
@@ -742,9 +744,10 @@ int sled_launch_copy_gain(int dtype, const void* src, float* dst, int n, hipStre
 int sled_launch_step_setup(const sled_model* m, const sled_kvpool* p, const sled_step_meta& meta, const int32_t* tokens, float* cs, int32_t* kvslot,
                            int32_t* plan, int32_t* arrive, float* h, void* X, size_t plane, const float* gain, hipStream_t st) {
     const bool bf = m->s.dtype == SLED_BF16;
-    step_setup a{p->len_dev, m->s.head_dim / 2, m->s.n_kv_heads, (double)m->s.rope_theta, reinterpret_cast<float2*>(cs), kvslot, plan, arrive,
-                 meta.B * m->s.n_kv_heads, tokens, m->embed, m->s.vocab, m->s.d_model, m->s.rms_eps, gain, h, X, plane, (meta.T + 3) / 4,
-                 bf ? (std::max(meta.n_work, meta.B * m->s.n_kv_heads) + 255) / 256 : 0};
+    const int n_arrive = meta.n_work > 0 ? meta.B * m->s.n_kv_heads : 0;   // (a step over trees has a plan of its own)
+    step_setup a{p->len_dev, p->shift_dev, m->s.head_dim / 2, m->s.n_kv_heads, (double)m->s.rope_theta, reinterpret_cast<float2*>(cs), kvslot, plan, arrive,
+                 n_arrive, tokens, m->embed, m->s.vocab, m->s.d_model, m->s.rms_eps, gain, h, X, plane, (meta.T + 3) / 4,
+                 bf ? (std::max(meta.n_work, n_arrive) + 255) / 256 : 0};
     const dim3 grid(a.rope_blocks + a.plan_blocks + meta.T);
     if (bf) hipLaunchKernelGGL(step_setup_kernel<true>, grid, dim3(256), 0, st, meta, a);
     else hipLaunchKernelGGL(step_setup_kernel<false>, grid, dim3(256), 0, st, meta, a);
@@ -849,19 +852,19 @@ int sled_launch_kv_export(const sled_model* m, const sled_kvpool* p, void* k_dst
     return launch_kv_move<false>(m, p, &pc, 1, st);
 }
 
-int sled_launch_len_add(int32_t* len_dev, const int32_t* req_ids_dev, const int32_t* add_dev, const int32_t* fresh_dev, const int32_t* accept_dev,
+int sled_launch_len_add(int32_t* len_dev, int32_t* shift_dev, const int32_t* req_ids_dev, const int32_t* add_dev, const int32_t* fresh_dev, const int32_t* accept_dev,
                         int B, hipStream_t st) {
-    hipLaunchKernelGGL(len_add_kernel, dim3((B + 63) / 64), dim3(64), 0, st, len_dev, req_ids_dev, add_dev, fresh_dev, accept_dev, B);
+    hipLaunchKernelGGL(len_add_kernel, dim3((B + 63) / 64), dim3(64), 0, st, len_dev, shift_dev, req_ids_dev, add_dev, fresh_dev, accept_dev, B);
     SLED_LAUNCH_CHECK();
     return SLED_OK;
 }
 
-int sled_launch_len_zero(int32_t* len_dev, const int* req_ids /*host*/, int n, hipStream_t st) {
+int sled_launch_len_zero(int32_t* len_dev, int32_t* shift_dev, const int* req_ids /*host*/, int n, hipStream_t st) {
     for (int i0 = 0; i0 < n; i0 += 128) {
         len_ids ids{};
         const int here = std::min(n - i0, 128);
         for (int i = 0; i < here; i++) ids.id[i] = req_ids[i0 + i];
-        hipLaunchKernelGGL(len_zero_kernel, dim3(1), dim3(128), 0, st, len_dev, ids, here);
+        hipLaunchKernelGGL(len_zero_kernel, dim3(1), dim3(128), 0, st, len_dev, shift_dev, ids, here);
         SLED_LAUNCH_CHECK();
     }
     return SLED_OK;

@@ -173,6 +173,24 @@ struct sled_request {
     std::vector<int> pages;
 };
 
+// A batch of draft trees, planned by sled_tree_begin: device arrays in the caller's workspace and the sizes of the launches over them
+constexpr int SLED_TREE_TILES = 4;   // row tiles of 16 that an attention work item covers at most
+constexpr int SLED_TREE_ITEM = 12;   // ints of an attention work item:
+//   [0] request id  [1] kv head  [2] first page  [3] pages  [4] nodes  [5] first packed row  [6] first entry of the request's page list
+//   [7] first item of this (request, kv head, row group)  [8] how many there are  [9] how far apart  [10] first stacked row  [11] has the tree
+struct sled_tree_plan {
+    const int32_t* items;        // [n_items][SLED_TREE_ITEM]
+    const int32_t* mass_items;   // [n_mass_items][8]  as [0] .. [6] above
+    const uint64_t* seen;        // [T] which nodes of its tree a node sees: its ancestors and itself
+    const int32_t* pages;        // the requests' page lists
+    int32_t* arrive;             // [n_items][4] arrival counter (zero between launches), -, nodes with values that are not finite
+    float* part_o;               // states of split items
+    float* part_ml;
+    int n_items, n_mass_items;
+    int tiles;                   // row tiles of 16 that a work item covers: 1, 2 or SLED_TREE_TILES
+    int max_nodes, T;
+};
+
 struct sled_kvpool {
     const sled_model* m;
     int64_t n_pages;
@@ -181,9 +199,19 @@ struct sled_kvpool {
     void* k_pool;              // [n_layers][n_pages][Hkv][16*D] in the layout of the dtype
     void* v_pool;
     int32_t* len_dev;          // [max_requests] committed context length of each request
+    int32_t* shift_dev;        // [max_requests] tokens evicted so far: how far positions run ahead of the length
     std::vector<sled_request> reqs;
     std::vector<int> free_pages;
     std::vector<int> last_batch;   // request ids of the last verify
+    // the trees at hand (sled_tree_begin); whatever changes one of their requests' lengths or pages ends the plan
+    struct tree_state {
+        bool valid = false;
+        sled_tree_plan plan;
+        const void* workspace = nullptr;
+        std::vector<int> reqs;
+        int max_reach = 0;         // the largest upper bound of context and nodes
+    };
+    tree_state tree;
     // ring of pinned-host + device staging buffers for per-call metadata (page lists, row maps)
     static const int RING = 8;
     struct stage_slot {
@@ -220,6 +248,7 @@ struct sled_step_meta {
     const int32_t* cu_pages;   // [B+1]
     const int32_t* row_req;    // [T]   index into the batch (not the request id)
     const int32_t* row_j;      // [T]   index of the row inside its request
+    const int32_t* row_depth;  // [T]   how many positions the row's token lies behind its block's first (row_j but for trees)
     const int32_t* pages;      // [sum pages]
     const int32_t* work;       // [n_work * 4]  attention work items: batch index, kv head, first page, n pages
     const int32_t* cu_work;    // [B*Hkv][2]    first work item of each (batch index, kv head) and their number; they lie Hkv places apart
@@ -270,9 +299,30 @@ int sled_launch_kv_ingest(const sled_model* m, const sled_kvpool* p, const sled_
 int sled_launch_kv_export(const sled_model* m, const sled_kvpool* p, void* k_dst, void* v_dst, int first, int n_tokens,
                           const int32_t* pages_dev, hipStream_t st);
 // fresh_dev (or nullptr): nonzero where a request starts from length zero
-int sled_launch_len_add(int32_t* len_dev, const int32_t* req_ids_dev, const int32_t* add_dev, const int32_t* fresh_dev, const int32_t* accept_dev,
+int sled_launch_len_add(int32_t* len_dev, int32_t* shift_dev, const int32_t* req_ids_dev, const int32_t* add_dev, const int32_t* fresh_dev, const int32_t* accept_dev,
                         int B, hipStream_t st);
-int sled_launch_len_zero(int32_t* len_dev, const int* req_ids /*host*/, int n, hipStream_t st);
+int sled_launch_len_zero(int32_t* len_dev, int32_t* shift_dev, const int* req_ids /*host*/, int n, hipStream_t st);
+
+// tree.hip
+int sled_launch_tree_attention(const sled_model* m, const sled_kvpool* p, const sled_tree_plan& t, int layer, const void* q, size_t q_stride, size_t q_plane,
+                               const void* k, size_t k_stride, const void* v, size_t v_stride, void* out, size_t x_plane, float* lse, bool step, hipStream_t st);
+int sled_launch_tree_mass(const sled_model* m, const sled_kvpool* p, const sled_tree_plan& t, int layer, const void* q, size_t q_stride, size_t q_plane,
+                          const float* lse, float* mass, int cap, hipStream_t st);
+int sled_launch_tree_qkv(const sled_model* m, int T, const float* partial, int n_split, int T_pad, const float* cs, void* Q, size_t q_plane, void* K, void* V,
+                         hipStream_t st);
+
+// evict.hip
+constexpr int SLED_EVICT_REC = 5;
+int sled_launch_evict(const sled_model* m, const sled_kvpool* p, const int32_t* meta, const int32_t* pages, int B, int keep_max, int first, int recent, float* mass,
+                      int cap, int32_t* idx, int idx_cap, bool in_place, hipStream_t st);
+int sled_launch_tree_commit(const sled_model* m, const sled_kvpool* p, const int32_t* meta, const int32_t* pages, int B, const int32_t* accept_len,
+                            const int32_t* path, float* mass, int cap, hipStream_t st);
+
+// accept_tree.hip
+size_t sled_accept_tree_ws_bytes(int B, int T, int vocab);
+// depth: of the deepest tree (0: roots only)
+int sled_launch_accept_tree(int mode, int B, int T, const int* n_nodes, const int* parent, int depth, int vocab, float temperature, const float* logits,
+                            const int32_t* tokens, const float* u, int32_t* accept_len, int32_t* path, int32_t* out_token, void* ws, hipStream_t st);
 
 // gemm.hip:  out = X[T, K] * W[N, K]^T
 enum { SLED_EPI_PARTIAL = 0, SLED_EPI_SWIGLU = 1, SLED_EPI_STORE = 2 };

@@ -79,6 +79,46 @@ class Verifier:
     def commit(self, reqs: Sequence[int], accept_len: torch.Tensor) -> None:
         sled.sled_kv_append(self.pool, reqs, accept_len=accept_len)
 
+    # ---- trees of drafts, a bounded cache -----------------------------------------------------
+    def enable_trees(self, nodes_max: int, ctx_tokens_max: int, mass_cap: int = 0, max_requests: int = 0) -> None:
+        """Buffers for steps over trees of up to nodes_max nodes on contexts of ctx_tokens_max tokens together.  mass_cap > 0: the weight that
+        attention gives the tokens of up to max_requests requests of up to mass_cap tokens (nodes included) is added up, for evict()."""
+        s, B = self.shape, self.B_max
+        T = B * nodes_max
+        self.tree_ws = sled.workspace(sled.sled_verify_tree_workspace_bytes(self.model, B, T, ctx_tokens_max + T))
+        self.tree_acc_ws = sled.workspace(sled.sled_accept_tree_workspace_bytes(B, T, s.vocab))
+        self.tree_logits = torch.empty(T, s.vocab, dtype=torch.float32, device="cuda")
+        self.path = torch.full((B, sled.TREE_MAX), -1, dtype=torch.int32, device="cuda")
+        self.mass = None
+        if mass_cap:
+            self.mass = torch.zeros(max_requests, s.n_layers, s.n_kv_heads, mass_cap, dtype=torch.float32, device="cuda")
+            self.evict_ws = sled.workspace(sled.sled_kv_evict_workspace_bytes(self.model, B, mass_cap))
+
+    def open_bounded(self) -> int:
+        """open(), with nothing yet in the request's rows of mass."""
+        r = self.open()
+        self.mass[r].zero_()
+        return r
+
+    def verify_tree(self, reqs: Sequence[int], parents: Sequence[Sequence[int]], tokens: torch.Tensor) -> torch.Tensor:
+        n = [len(p) for p in parents]
+        out = self.tree_logits[: sum(n)]
+        sled.sled_verify_tree(self.model, self.pool, reqs, n, parents, tokens, out, self.tree_ws, self.mass)
+        return out
+
+    def accept_tree(self, mode: int, parents: Sequence[Sequence[int]], logits: torch.Tensor, tokens: torch.Tensor, u: Optional[torch.Tensor] = None,
+                    temperature: float = 1.0):
+        B = len(parents)
+        sled.sled_accept_tree(mode, [len(p) for p in parents], parents, self.shape.vocab, temperature, logits, tokens, u, self.accept_len[:B], self.path[:B],
+                              self.out_token[:B], self.tree_acc_ws)
+        return self.accept_len[:B], self.path[:B], self.out_token[:B]
+
+    def commit_tree(self, reqs: Sequence[int], accept_len: torch.Tensor, path: torch.Tensor) -> None:
+        sled.sled_tree_commit(self.pool, reqs, accept_len, path, self.mass)
+
+    def evict(self, reqs: Sequence[int], keep: Sequence[int], n_first: int, n_recent: int) -> None:
+        sled.sled_kv_evict(self.pool, reqs, keep, n_first, n_recent, self.mass, self.evict_ws)
+
     def read_kv(self, req: int, first_token: int, n_tokens: int):
         """K and V of positions first_token .. first_token + n_tokens - 1 as stored, each [n_layers, n_tokens, n_kv_heads, head_dim]."""
         s = self.shape

@@ -24,6 +24,10 @@ sled_accept and sled_kv_append.  The pieces:
   SamplingDrafter stands in for a device that drafts by sampling: every draft comes with the distribution it was
                   drawn from (dense, or its top entries as (id, probability) pairs), which is what the server's
                   sampling mode (Eq. 1, seeded uniforms per device and round) verifies against.
+  Trees           a server made with trees=True takes drafts that branch (submit's `parents`): the step then is
+                  sled_verify_tree, sled_accept_tree and sled_tree_commit, and an answer carries the accepted path.  With
+                  kv_budget it also keeps every session's cache below that many tokens (sled_kv_evict).
+                  TreeDrafter stands in for a device that drafts such trees.
   simulate        devices draft for an exponentially distributed time (mean k x per-token draft
                   time), queue at the server, wait for the batch to fill, get their answer after the
                   measured GPU time of the step; virtual clock, real GPU work.
@@ -56,6 +60,8 @@ class Pending:
     # speculative sampling only: the distributions the drafts were drawn from, one row per draft -- dense
     # float32 [k, vocab], or sparse as (token ids int32 [k, m], probabilities float32 [k, m]); on the GPU
     q: Optional[object] = None
+    # trees only: the node that each draft continues (node 0 is the pending token, draft j is node j + 1); None is a chain
+    parents: Optional[List[int]] = None
 
 
 @dataclasses.dataclass
@@ -65,18 +71,34 @@ class Response:
     accept_len: int
     out_token: int
     replayed: bool = False   # answered from the record of an earlier, lost answer
+    path: Optional[List[int]] = None   # trees: the accepted drafts' nodes in order (node j is draft j - 1)
+
+    def accepted(self, drafts: Sequence[int]) -> List[int]:
+        """The accepted tokens among the round's drafts."""
+        return list(drafts[: self.accept_len]) if self.path is None else [drafts[j - 1] for j in self.path]
 
 
 class Server:
     """Queue + static batch planner + the verification step for a set of devices."""
 
     def __init__(self, verifier: Verifier, batch_size: int, device: str = "cuda", mode: str = "greedy",
-                 temperature: float = 1.0, seed: int = 0):
-        """mode "greedy": exact match against the target's argmax chain.  mode "sample": speculative sampling
+                 temperature: float = 1.0, seed: int = 0, trees: bool = False, kv_budget: int = 0, kv_keep: int = 0, kv_first: int = 4,
+                 kv_recent: int = 64):
+        """trees (needs Verifier.enable_trees): every round is a step over trees; sampling mode then names each node's token with a uniform
+        of its own and needs no draft distributions.  kv_budget > 0 (trees, and a Verifier that adds up mass): a session whose cache holds
+        more tokens after a round is cut to kv_keep (default: three quarters of the budget), its first kv_first and last kv_recent
+        tokens among them; a session must not open with more.
+        mode "greedy": exact match against the target's argmax chain.  mode "sample": speculative sampling
         (Eq. 1): every request carries the distributions its drafts were drawn from, and the uniforms of a round
         are a function of (seed, device, round number) alone, so an answer does not depend on how the round
         was batched and a retried round draws the same numbers."""
         assert mode in ("greedy", "sample")
+        assert trees or not kv_budget
+        self.trees, self.kv_budget, self.kv_keep = trees, kv_budget, kv_keep or max(1, 3 * kv_budget // 4)
+        self.kv_first, self.kv_recent = kv_first, kv_recent
+        assert not kv_budget or (kv_first + kv_recent <= self.kv_keep <= kv_budget and getattr(verifier, "mass", None) is not None)
+        self.length: Dict[int, int] = {}              # device -> tokens in its cache (kept where a budget needs it)
+        self.evictions = 0
         self.v = verifier
         self.batch_size = batch_size
         self.device = device        # where the packed token ids of a step are put
@@ -98,7 +120,11 @@ class Server:
         its K/V ([layers, tokens, kv heads, head dim], model dtype, on the GPU), or the prompt tokens themselves,
         which then run through the target model into the cache (sled_prefill)."""
         assert device not in self.req_of
-        r = self.v.open()
+        if self.kv_budget:
+            n = (K.shape[1] if K is not None else 0) + (len(prompt) if prompt is not None else 0)
+            assert n <= self.kv_budget, "the session opens with more tokens than the cache may hold"
+            self.length[device] = n
+        r = self.v.open_bounded() if self.kv_budget else self.v.open()
         self.req_of[device] = r
         if K is not None and K.shape[1] > 0:
             self.v.append_context([r], [K], [V])
@@ -108,18 +134,29 @@ class Server:
     def close(self, device: int) -> None:
         self.v.close_request(self.req_of.pop(device))
         self.last.pop(device, None)
+        self.length.pop(device, None)
         self.queue = collections.deque(p for p in self.queue if p.device != device)
 
     # ---- requests ---------------------------------------------------------------------------
-    def submit(self, device: int, round_no: int, pending_token: int, drafts: Sequence[int], q=None) -> Optional[Response]:
+    def submit(self, device: int, round_no: int, pending_token: int, drafts: Sequence[int], q=None,
+               parents: Optional[Sequence[int]] = None) -> Optional[Response]:
         """Queue a verification request.  A round the server has already verified (the device did not get the
         answer and sent it again, possibly with more drafts) is answered at once from the record.  In sampling
-        mode q holds the draft distributions (see Pending)."""
+        mode q holds the draft distributions, on a server of trees parents the node that each draft continues (see Pending)."""
         last = self.last.get(device)
         if last is not None and round_no <= last.round_no:
             if round_no < last.round_no:
                 raise ValueError(f"device {device}: round {round_no} is older than the last answered round {last.round_no}")
             return dataclasses.replace(last, replayed=True)
+        if self.trees:
+            drafts = [int(d) for d in drafts][: sled.TREE_MAX - 1]
+            up = list(range(len(drafts))) if parents is None else [int(x) for x in parents][: len(drafts)]
+            if len(up) != len(drafts) or any(not 0 <= x <= j for j, x in enumerate(up)):
+                raise ValueError(f"device {device}: every draft continues a node that comes before it")
+            self.queue.append(Pending(device, round_no, int(pending_token), drafts, None, up))
+            return None
+        if parents is not None:
+            raise ValueError("this server takes chains of drafts (trees=True takes trees)")
         if len(drafts) > self.v.shape.k_max:
             drafts = drafts[: self.v.shape.k_max]   # the rest is drafted again next round
         if self.mode == "sample":
@@ -153,6 +190,8 @@ class Server:
             seen.add(p.device)
             batch.append(p)
         self.queue.extendleft(reversed(rest))
+        if self.trees:
+            return self._run_trees(batch)
         reqs = [self.req_of[p.device] for p in batch]
         k = [len(p.drafts) for p in batch]
         toks: List[int] = []
@@ -202,6 +241,42 @@ class Server:
         return out
 
 
+    def _run_trees(self, batch: List[Pending]) -> List[Response]:
+        reqs = [self.req_of[p.device] for p in batch]
+        parents = [[-1] + p.parents for p in batch]
+        toks: List[int] = []
+        for p in batch:
+            toks += [p.pending_token] + p.drafts
+        tokens = torch.tensor(toks, dtype=torch.int32, device=self.device)
+        logits = self.v.verify_tree(reqs, parents, tokens)
+        u = None
+        if self.mode == "sample":   # a uniform per node, a function of (seed, device, round number) like the others
+            u = torch.from_numpy(np.concatenate([self.round_uniforms(p.device, p.round_no, len(p.drafts) + 1)[0] for p in batch])).to(self.device)
+        a, path, t = self.v.accept_tree(sled.SAMPLE if u is not None else sled.GREEDY, parents, logits, tokens, u, self.temperature)
+        self.v.commit_tree(reqs, a, path)
+        if self.observer is not None:
+            self.observer(dict(batch=batch, parents=parents, tokens=tokens, logits=logits, accept_len=a, path=path, out_token=t, u=u))
+        a_h, p_h, t_h = a.cpu().tolist(), path.cpu().tolist(), t.cpu().tolist()
+        out = []
+        for p, ai, pi, ti in zip(batch, a_h, p_h, t_h):
+            r = Response(p.device, p.round_no, int(ai), int(ti), path=pi[:ai])
+            self.last[p.device] = r
+            out.append(r)
+        if self.kv_budget:
+            for p, ai in zip(batch, a_h):
+                self.length[p.device] += ai + 1
+            full = [p.device for p in batch if self.length[p.device] > self.kv_budget]
+            if full:
+                self.v.evict([self.req_of[d] for d in full], [self.kv_keep] * len(full), self.kv_first, self.kv_recent)
+                for d in full:
+                    self.length[d] = self.kv_keep
+                self.evictions += len(full)
+        self.steps += 1
+        self.rows += len(toks)
+        self.drafts_seen += len(toks) - len(batch)
+        return out
+
+
 class ReplayDrafter:
     """Draft tokens for a device whose target continuation is known: token j of a draft is the true next token
     with probability beta (as long as all earlier ones were), anything else afterwards."""
@@ -226,6 +301,37 @@ class ReplayDrafter:
                     wrong = (wrong + 1) % self.vocab
                 out.append(wrong)
         return out
+
+
+class TreeDrafter(ReplayDrafter):
+    """ReplayDrafter for trees: k levels of `width` guesses each; every level's guesses continue the level before's best one.  The true token is
+    the best guess with probability beta, else, half the time, one of the others (only then the tree beats a chain), from which nothing
+    is drafted further."""
+
+    def __init__(self, truth: Sequence[int], vocab: int, beta: float, seed: int, width: int):
+        super().__init__(truth, vocab, beta, seed)
+        self.width = width
+
+    def draft_tree(self, n_done: int, k: int) -> Tuple[List[int], List[int]]:
+        drafts: List[int] = []
+        parents: List[int] = []
+        up, good = 0, True
+        k = min(k, (sled.TREE_MAX - 1) // self.width)
+        for j in range(k):
+            pos = n_done + j
+            true = self.truth[pos] if pos < len(self.truth) else -1
+            level = [int(x) for x in self.rng.integers(0, self.vocab, size=self.width)]
+            level = [(x + 1) % self.vocab if x == true else x for x in level]
+            hit = good and true >= 0 and self.rng.random() < self.beta
+            if hit:
+                level[0] = true
+            elif good and true >= 0 and self.width > 1 and self.rng.random() < 0.5:
+                level[int(self.rng.integers(1, self.width))] = true
+            good = hit
+            drafts += level
+            parents += [up] * self.width
+            up = j * self.width + 1     # node of the level's best guess
+        return drafts, parents
 
 
 class SamplingDrafter:
@@ -301,19 +407,22 @@ def simulate(server: Server, drafters: Dict[int, ReplayDrafter], first_tokens: D
     def send(d: int, t: float) -> None:
         nonlocal tie
         kk = min(k, max(0, n_new - len(texts[d]) - 1))
-        if hasattr(drafters[d], "draft_with_q"):
+        parents = None
+        if hasattr(drafters[d], "draft_tree"):
+            (drafts, parents), q = drafters[d].draft_tree(len(texts[d]), kk), None
+        elif hasattr(drafters[d], "draft_with_q"):
             drafts, q = drafters[d].draft_with_q(len(texts[d]), kk)
         else:
             drafts, q = drafters[d].draft(len(texts[d]), kk), None
-        sent[d] = Pending(d, rounds[d], pend[d], drafts, q)
-        r = server.submit(d, rounds[d], pend[d], drafts, q)
+        sent[d] = Pending(d, rounds[d], pend[d], drafts, q, parents)
+        r = server.submit(d, rounds[d], pend[d], drafts, q, parents)
         assert r is None
 
     def apply(r: Response, t: float) -> None:
         nonlocal tie
         d = r.device
         p = sent.pop(d)
-        texts[d] += p.drafts[: r.accept_len] + [r.out_token]
+        texts[d] += r.accepted(p.drafts) + [r.out_token]
         pend[d] = r.out_token
         rounds[d] += 1
         if drafters[d].truth is not None and texts[d] != drafters[d].truth[: len(texts[d])]:
@@ -349,7 +458,8 @@ def simulate(server: Server, drafters: Dict[int, ReplayDrafter], first_tokens: D
             answers += 1
             if lose_every and answers % lose_every == 0:
                 # the answer is lost; the device's timer fires and it sends the same round again
-                again = server.submit(r.device, r.round_no, sent[r.device].pending_token, sent[r.device].drafts, sent[r.device].q)
+                again = server.submit(r.device, r.round_no, sent[r.device].pending_token, sent[r.device].drafts, sent[r.device].q,
+                                      sent[r.device].parents)
                 assert again is not None and again.replayed and (again.accept_len, again.out_token) == (r.accept_len, r.out_token)
                 r = again
             apply(r, now)
@@ -377,6 +487,8 @@ def main() -> None:
                     help="make a request's logits independent of its batch to the last bit (sled_model_set_batch_invariant)")
     ap.add_argument("--weights", default="bf16", choices=["bf16", "fp8", "fp4"],
                     help="projection weight format of the target (sled_model_set_weight_bits)")
+    ap.add_argument("--tree-width", type=int, default=0, help="devices draft trees of k levels with so many guesses each (0: chains)")
+    ap.add_argument("--kv-budget", type=int, default=0, help="tokens a session's cache may hold; beyond, those with the least attention go")
     ap.add_argument("--sweep", action="store_true", help="run batch sizes 4..32 x k in {2, 4, 8} instead of --batch/--k")
     args = ap.parse_args()
     sled.lib()
@@ -391,7 +503,12 @@ def main() -> None:
         shape, seed=args.seed, device="cuda")
     v = Verifier(shape, weights, budget // 16 + 3 * args.devices + 8, args.devices, args.devices, budget,
                  batch_invariant=args.batch_invariant)
-    server = Server(v, args.batch)
+    trees = bool(args.tree_width or args.kv_budget)
+    if trees:
+        nodes = min(sled.TREE_MAX, 1 + max(1, args.tree_width) * max(args.k, 8 if args.sweep else 0))
+        ctx = [min(c, args.kv_budget) for c in ctx] if args.kv_budget else ctx
+        v.enable_trees(nodes, budget, args.kv_budget + 2 * nodes if args.kv_budget else 0, args.devices)
+    server = Server(v, args.batch, trees=trees, kv_budget=args.kv_budget)
     devs = list(range(args.devices))
     first = [int(x) for x in rng.integers(0, shape.vocab, size=args.devices)]
     KV = [synth.context_kv(shape, ctx[d], seed=args.seed, req=d, device="cuda") for d in devs]
@@ -409,12 +526,17 @@ def main() -> None:
         server.batch_size = batch
         for d in devs:
             server.open(d, *KV[d])
-        drafters = {d: ReplayDrafter(truth[d], shape.vocab, args.beta, seed=args.seed * 1000 + d) for d in devs}
+        if args.tree_width:
+            drafters = {d: TreeDrafter(truth[d], shape.vocab, args.beta, args.seed * 1000 + d, args.tree_width) for d in devs}
+        else:
+            drafters = {d: ReplayDrafter(truth[d], shape.vocab, args.beta, seed=args.seed * 1000 + d) for d in devs}
         res = simulate(server, drafters, dict(zip(devs, first)), args.tokens, min(k, shape.k_max), args.draft_ms, seed=args.seed)
         ok = ok and res["devices_off_replayed_path"] == 0
         res.pop("texts")
         res.update({"shape": args.shape, "layers": shape.n_layers, "devices": args.devices, "batch": batch, "k": k,
                     "beta": args.beta, "draft_ms_per_token": args.draft_ms, "mean_context": int(np.mean(ctx)), "batch_invariant": args.batch_invariant})
+        if trees:
+            res.update({"tree_width": args.tree_width, "kv_budget": args.kv_budget, "evictions": server.evictions})
         print(json.dumps({k_: (round(x, 3) if isinstance(x, float) else x) for k_, x in res.items()}), flush=True)
     v.destroy()
     if not ok:

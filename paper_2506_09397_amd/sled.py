@@ -34,8 +34,12 @@ EXPORTS = [
     "sled_kv_append", "sled_kv_read", "sled_verify_workspace_bytes", "sled_verify_batch", "sled_prefill",
     "sled_attention_partition", "sled_projection_slices", "sled_projection_rows",
     "sled_accept_workspace_bytes", "sled_accept", "sled_accept_static", "sled_accept_sparse", "sled_row_confidence", "sled_profile_enable", "sled_profile_read",
+    "sled_tree_workspace_bytes", "sled_tree_begin", "sled_tree_attention", "sled_tree_mass", "sled_tree_commit",
+    "sled_verify_tree_workspace_bytes", "sled_verify_tree", "sled_accept_tree_workspace_bytes", "sled_accept_tree",
+    "sled_kv_evict_workspace_bytes", "sled_kv_evict", "sled_kvpool_positions",
     "sled_strerror", "sled_last_error",
 ]
+TREE_MAX = 64   # nodes of a draft tree
 PROF_PROJ, PROF_ATTN, PROF_ROWS, PROF_N = 0, 1, 2, 3
 
 
@@ -88,6 +92,22 @@ def lib() -> C.CDLL:
     L.sled_accept_static.argtypes = [C.c_int, C.c_int, ip, C.c_int, C.c_float, vp, vp, vp, vp, vp, vp, vp, vp]
     L.sled_accept_sparse.argtypes = [C.c_int, ip, C.c_int, C.c_float, vp, vp, C.c_int, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     L.sled_row_confidence.argtypes = [C.c_int, C.c_int, C.c_float, vp, vp, vp, vp, C.c_size_t, vp]
+    L.sled_tree_workspace_bytes.argtypes = [vp, C.c_int, C.c_int, C.c_int64]
+    L.sled_tree_workspace_bytes.restype = C.c_size_t
+    L.sled_tree_begin.argtypes = [vp, C.c_int, ip, ip, ip, vp, C.c_size_t, vp]
+    L.sled_tree_attention.argtypes = [vp, C.c_int, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, vp, vp, vp, vp]
+    L.sled_tree_mass.argtypes = [vp, C.c_int, vp, C.c_int64, vp, vp, C.c_int, vp, vp]
+    L.sled_tree_commit.argtypes = [vp, C.c_int, ip, vp, vp, vp, C.c_int, vp]
+    L.sled_verify_tree_workspace_bytes.argtypes = [vp, C.c_int, C.c_int, C.c_int64]
+    L.sled_verify_tree_workspace_bytes.restype = C.c_size_t
+    L.sled_verify_tree.argtypes = [vp, vp, C.c_int, ip, ip, ip, vp, vp, vp, C.c_int, vp, C.c_size_t, vp]
+    L.sled_accept_tree_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
+    L.sled_accept_tree_workspace_bytes.restype = C.c_size_t
+    L.sled_accept_tree.argtypes = [C.c_int, C.c_int, ip, ip, C.c_int, C.c_float, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.sled_kv_evict_workspace_bytes.argtypes = [vp, C.c_int, C.c_int]
+    L.sled_kv_evict_workspace_bytes.restype = C.c_size_t
+    L.sled_kv_evict.argtypes = [vp, C.c_int, ip, ip, ip, C.c_int, C.c_int, vp, C.c_int, vp, C.c_size_t, vp]
+    L.sled_kvpool_positions.argtypes = [vp, C.c_int, ip, ip, vp]
     L.sled_profile_enable.argtypes = [vp, C.c_int]
     L.sled_profile_read.argtypes = [vp, vp, C.POINTER(C.c_float), ip]
     L.sled_strerror.argtypes = [C.c_int]
@@ -278,6 +298,102 @@ def sled_profile_read(model: int):
     n = (C.c_int * PROF_N)()
     _check(lib().sled_profile_read(model, _stream(), ms, n))
     return list(ms), list(n)
+
+
+# ---------------------------------------------------------------------------------------- trees of drafts, eviction
+def _parents(n_nodes: Sequence[int], parents: Sequence[Sequence[int]]):
+    """parents[i][j]: the node that node j of tree i continues (parents[i][0] is not looked at), packed."""
+    assert len(parents) == len(n_nodes) and all(len(p) == n for p, n in zip(parents, n_nodes)), "a parent for every node of every tree"
+    return _ints([max(int(x), -1) if j else -1 for p in parents for j, x in enumerate(p)])
+
+
+def _rows(t: torch.Tensor):
+    """(pointer, elements between rows) of a [T, heads, head_dim] tensor whose rows may lie apart."""
+    assert t.is_cuda and t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2], "rows of [heads, head_dim], each contiguous"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _bytes(t: torch.Tensor) -> int:
+    return t.numel() * t.element_size()
+
+
+def _mass(mass: Optional[torch.Tensor]):
+    """(pointer, entries of a row) of a [max_requests, n_layers, n_kv_heads, cap] float32 tensor."""
+    if mass is None:
+        return None, 0
+    assert mass.dtype == torch.float32 and mass.dim() == 4
+    return _ptr(mass), int(mass.shape[3])
+
+
+def sled_tree_workspace_bytes(model: int, B_max: int, T_max: int, ctx_tokens_max: int) -> int:
+    return int(lib().sled_tree_workspace_bytes(model, B_max, T_max, ctx_tokens_max))
+
+
+def sled_tree_begin(pool: int, req_ids: Sequence[int], n_nodes: Sequence[int], parents: Sequence[Sequence[int]], workspace: torch.Tensor) -> None:
+    assert len(req_ids) == len(n_nodes)
+    _check(lib().sled_tree_begin(pool, len(req_ids), _ints(req_ids), _ints(n_nodes), _parents(n_nodes, parents), _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def sled_tree_attention(pool: int, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor],
+                        workspace: torch.Tensor) -> None:
+    assert q.dtype == k.dtype == v.dtype == out.dtype and (lse is None or lse.dtype == torch.float32)
+    assert q.shape[0] == k.shape[0] == v.shape[0] and k.shape == v.shape and out.shape == q.shape and (lse is None or lse.shape == q.shape[:2])
+    _check(lib().sled_tree_attention(pool, int(layer), *_rows(q), *_rows(k), *_rows(v), _ptr(out), _ptr(lse), _ptr(workspace), _stream()))
+
+
+def sled_tree_mass(pool: int, layer: int, q: torch.Tensor, lse: torch.Tensor, mass: torch.Tensor, workspace: torch.Tensor) -> None:
+    assert lse.dtype == torch.float32 and lse.shape == q.shape[:2]
+    _check(lib().sled_tree_mass(pool, int(layer), *_rows(q), _ptr(lse), *_mass(mass), _ptr(workspace), _stream()))
+
+
+def sled_tree_commit(pool: int, req_ids: Sequence[int], accept_len: torch.Tensor, path: torch.Tensor, mass: Optional[torch.Tensor] = None) -> None:
+    assert accept_len.dtype == torch.int32 and path.dtype == torch.int32 and tuple(path.shape) == (len(req_ids), TREE_MAX) and accept_len.numel() == len(req_ids)
+    _check(lib().sled_tree_commit(pool, len(req_ids), _ints(req_ids), _ptr(accept_len), _ptr(path), *_mass(mass), _stream()))
+
+
+def sled_verify_tree_workspace_bytes(model: int, B_max: int, T_max: int, ctx_tokens_max: int) -> int:
+    return int(lib().sled_verify_tree_workspace_bytes(model, B_max, T_max, ctx_tokens_max))
+
+
+def sled_verify_tree(model: int, pool: int, req_ids: Sequence[int], n_nodes: Sequence[int], parents: Sequence[Sequence[int]], tokens: torch.Tensor,
+                     logits: torch.Tensor, workspace: torch.Tensor, mass: Optional[torch.Tensor] = None) -> None:
+    assert tokens.dtype == torch.int32 and logits.dtype == torch.float32 and len(req_ids) == len(n_nodes)
+    assert tokens.numel() == sum(n_nodes) and logits.shape[0] == sum(n_nodes)
+    _check(lib().sled_verify_tree(model, pool, len(req_ids), _ints(req_ids), _ints(n_nodes), _parents(n_nodes, parents), _ptr(tokens), _ptr(logits), *_mass(mass),
+                                  _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def sled_accept_tree_workspace_bytes(B: int, T: int, vocab: int) -> int:
+    return int(lib().sled_accept_tree_workspace_bytes(B, T, vocab))
+
+
+def sled_accept_tree(mode: int, n_nodes: Sequence[int], parents: Sequence[Sequence[int]], vocab: int, temperature: float, logits: torch.Tensor,
+                     tokens: torch.Tensor, u: Optional[torch.Tensor], accept_len: torch.Tensor, path: torch.Tensor, out_token: torch.Tensor,
+                     workspace: torch.Tensor) -> None:
+    T = sum(n_nodes)
+    assert logits.dtype == torch.float32 and tuple(logits.shape) == (T, vocab) and tokens.dtype == torch.int32 and tokens.numel() == T
+    assert u is None or (u.dtype == torch.float32 and u.numel() == T)
+    assert accept_len.dtype == torch.int32 and out_token.dtype == torch.int32 and path.dtype == torch.int32 and tuple(path.shape) == (len(n_nodes), TREE_MAX)
+    assert accept_len.numel() == out_token.numel() == len(n_nodes)
+    _check(lib().sled_accept_tree(mode, len(n_nodes), _ints(n_nodes), _parents(n_nodes, parents), vocab, float(temperature), _ptr(logits), _ptr(tokens), _ptr(u),
+                                  _ptr(accept_len), _ptr(path), _ptr(out_token), _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def sled_kv_evict_workspace_bytes(model: int, B_max: int, keep_max: int) -> int:
+    return int(lib().sled_kv_evict_workspace_bytes(model, B_max, keep_max))
+
+
+def sled_kv_evict(pool: int, req_ids: Sequence[int], keep: Sequence[int], n_first: int, n_recent: int, mass: torch.Tensor, workspace: torch.Tensor,
+                  dst_ids: Optional[Sequence[int]] = None) -> None:
+    assert len(keep) == len(req_ids) and (dst_ids is None or len(dst_ids) == len(req_ids))
+    _check(lib().sled_kv_evict(pool, len(req_ids), _ints(req_ids), None if dst_ids is None else _ints(dst_ids), _ints(keep), int(n_first), int(n_recent),
+                               *_mass(mass), _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def sled_kvpool_positions(pool: int, req_ids: Sequence[int]):
+    out = (C.c_int * len(req_ids))()
+    _check(lib().sled_kvpool_positions(pool, len(req_ids), _ints(req_ids), out, _stream()))
+    return list(out)
 
 
 # ---------------------------------------------------------------------------------------- helpers
