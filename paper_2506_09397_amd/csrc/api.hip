@@ -1276,7 +1276,8 @@ constexpr int MASS_ITEM_PAGES = 32;   // of a workgroup of the mass kernel: four
 struct tree_layout {
     size_t mass_items, seen, pages, arrive, ints, part_o, part_ml, total;   // byte offsets; the first `ints` bytes come from the host
 };
-tree_layout tree_plan_layout(const sled_model* m, int64_t n_items, int64_t n_mass, int T, int64_t n_pages, int tiles) {
+// n_slots: row tiles of all items
+tree_layout tree_plan_layout(const sled_model* m, int64_t n_items, int64_t n_slots, int64_t n_mass, int T, int64_t n_pages) {
     tree_layout w;
     size_t off = align_up((size_t)n_items * SLED_TREE_ITEM * 4, 16);
     w.mass_items = off;
@@ -1290,26 +1291,25 @@ tree_layout tree_plan_layout(const sled_model* m, int64_t n_items, int64_t n_mas
     w.ints = off;
     off = align_up(off, 256);
     w.part_o = off;
-    off += align_up((size_t)n_items * tiles * 16 * m->s.head_dim * sizeof(float), 256);
+    off += align_up((size_t)n_slots * 16 * m->s.head_dim * sizeof(float), 256);
     w.part_ml = off;
-    off += align_up((size_t)n_items * 2 * tiles * 16 * sizeof(float), 256);
+    off += align_up((size_t)n_slots * 2 * 16 * sizeof(float), 256);
     w.total = off;
     return w;
 }
 
+// work items of the tree attention: more than so many beyond one for every (request, row group, kv head) are never made
+int64_t tree_item_cap(int64_t groups, int Hkv) { return groups * Hkv + 3 * ATTN_CUS; }
+
 size_t tree_plan_bytes(const sled_model* m, int B, int T, int64_t ctx_tokens) {
+    constexpr int GROUP = 16 * SLED_TREE_TILES;
     const int Hkv = m->s.n_kv_heads, G = m->s.n_q_heads / Hkv;
     const int64_t n_pages = ctx_tokens / 16 + 2 * (int64_t)B, n_mass = Hkv * (n_pages / MASS_ITEM_PAGES + B);
-    size_t worst = 0;
-    for (int tiles = 1; tiles <= SLED_TREE_TILES; tiles *= 2) {
-        // (request, row group) pairs: several groups only where the most tiles do not hold a request's rows
-        constexpr int GROUP = 16 * SLED_TREE_TILES;
-        const int64_t groups = tiles < SLED_TREE_TILES ? B : std::min<int64_t>((int64_t)B * ceil_div(SLED_TREE_MAX * G, GROUP), B + (int64_t)T * G / GROUP);
-        int64_t items = attn_item_cap((int)groups, Hkv) + groups * Hkv;
-        if (m->batch_invariant) items = std::max(items, (ctx_tokens / (16 * SLED_FIXED_CHUNK_PAGES) + B) * Hkv * ceil_div((int)groups, B));
-        worst = std::max(worst, tree_plan_layout(m, items, n_mass, T, n_pages, tiles).total);
-    }
-    return worst;
+    const int64_t groups = std::min<int64_t>((int64_t)B * ceil_div(SLED_TREE_MAX * G, GROUP), B + (int64_t)T * G / GROUP);
+    // (runs of more than SLED_TREE_RUN pages are cut whatever the cap)
+    int64_t items = tree_item_cap(groups, Hkv) + ceil_div(n_pages, SLED_TREE_RUN / 2) * Hkv * ceil_div(groups, B);
+    if (m->batch_invariant) items = std::max(items, (ctx_tokens / (16 * SLED_FIXED_CHUNK_PAGES) + B) * Hkv * ceil_div(groups, B));
+    return tree_plan_layout(m, items, items * SLED_TREE_TILES, n_mass, T, n_pages).total;
 }
 
 int check_trees(int B, const int* n_nodes, const int* parent, int* T_out, int* depth_out, std::vector<int>* depths, const char* who) {
@@ -1333,29 +1333,41 @@ int check_trees(int B, const int* n_nodes, const int* parent, int* T_out, int* d
     return SLED_OK;
 }
 
-// Pages of a work item of the tree attention: every (request, kv head, row group) splits its context evenly into items of at most so many.
-// A launch of no more items than CUs takes as long as its longest; a longer one about its share of the whole on each CU and some of an item
-// more.  An item's own start and end count as ITEM_FIXED pages and, where its context is split, ITEM_SPLIT more.
-int tree_pages_per_item(const std::vector<int>& np, const std::vector<int>& groups, int Hkv) {
-    constexpr int ITEM_FIXED = 24, ITEM_SPLIT = 12, LEAST = 16;
+// The row tiles of a request that one pass over its context serves, and what a page costs such a pass
+struct tree_group {
+    int req, tile0, tiles, waves;
+    int pages;   // of context
+};
+// Wavefronts that share n row tiles; what is over works on other steps at the same time.
+int tree_waves(int n) { return n <= 2 ? 2 : n <= 4 ? 4 : 8; }
+// Time of a page in 1/16ths of one with all wavefronts on one step.
+int tree_page_cost(int waves) { return waves == 8 ? 16 : waves == 4 ? 10 : 7; }
+int tree_chunk(const tree_group& x, int tgt, int P) {
+    const int most = std::min(std::max(tgt * 16 / tree_page_cost(x.waves), P), SLED_TREE_RUN);
+    return ceil_div(attn_chunk(std::max(x.pages, 1), most), P) * P;   // a step of the kernel is P pages
+}
+
+// How long a work item of the tree attention may be, in pages of a pass with all wavefronts on one step: every group splits its context evenly into
+// items of at most so long.  A launch of no more items than CUs takes as long as its longest; a longer one about its share of the whole on each CU and
+// half a longest item more.  An item's own start and end count as ITEM_FIXED pages and, where its context is split, ITEM_SPLIT more.
+int tree_item_length(const std::vector<tree_group>& groups, int Hkv, int P) {
+    constexpr int ITEM_FIXED = 12, ITEM_SPLIT = 6, LEAST = 8;
     int longest = 1;
-    for (int n : np) longest = std::max(longest, n);
+    for (const tree_group& x : groups) longest = std::max(longest, ceil_div(x.pages * tree_page_cost(x.waves), 16));
     int best = longest;
     double best_end = -1.0;
-    for (int pieces = 1; pieces <= 64; pieces += std::max(1, pieces / 4)) {
-        const int tgt = ceil_div(longest, pieces);
-        if (pieces > 1 && tgt < LEAST) break;
-        int64_t items = 0, total = 0;
-        for (size_t i = 0; i < np.size(); i++) {
-            const int64_t n = std::max(1, ceil_div(np[i], tgt)), mult = (int64_t)groups[i] * Hkv;
-            items += mult * n;
-            total += mult * (np[i] + n * (ITEM_FIXED + (n > 1 ? ITEM_SPLIT : 0)));
+    for (int tgt = longest; tgt == longest || tgt >= LEAST; tgt = std::min(tgt - 1, tgt * 7 / 8)) {
+        int64_t items = 0;
+        double total = 0.0, most = 0.0;
+        for (const tree_group& x : groups) {
+            const int chunk = tree_chunk(x, tgt, P), runs = std::max(1, ceil_div(x.pages, chunk));
+            const double one = chunk * tree_page_cost(x.waves) / 16.0 + ITEM_FIXED + (runs > 1 ? ITEM_SPLIT : 0);
+            items += (int64_t)Hkv * runs;
+            total += Hkv * (x.pages * tree_page_cost(x.waves) / 16.0 + runs * (one - chunk * tree_page_cost(x.waves) / 16.0));
+            most = std::max(most, one);
         }
-        int64_t pairs = 0;
-        for (int g : groups) pairs += (int64_t)g;
-        if (items > attn_item_cap((int)pairs, Hkv)) break;
-        const double one = tgt + ITEM_FIXED + (pieces > 1 ? ITEM_SPLIT : 0), share = (double)total / ATTN_CUS;
-        const double end = items <= ATTN_CUS ? one : std::max(one, share) + 0.5 * total / items;
+        if (tgt < longest && items > tree_item_cap((int64_t)groups.size(), Hkv)) break;
+        const double end = items <= ATTN_CUS ? most : std::max(most, total / ATTN_CUS + 0.5 * most);
         if (best_end < 0 || end < best_end) {
             best_end = end;
             best = tgt;
@@ -1371,7 +1383,8 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
     const int Hkv = m->s.n_kv_heads, G = m->s.n_q_heads / Hkv, P = m->s.dtype == SLED_BF16 ? 2 : 1;
     int rc, T = 0, nmax = 0, reach_max = 0;
     int64_t n_pages = 0;
-    std::vector<int> np(B);   // context pages
+    std::vector<int> np(B), at_group(B + 1);   // context pages; first group
+    std::vector<tree_group> groups;
     for (int i = 0; i < B; i++) {
         const sled_request& rq = p->reqs[req_ids[i]];
         if ((rc = ensure_pages(p, req_ids[i], rq.len_ub + n_nodes[i])) != SLED_OK) return rc;
@@ -1381,22 +1394,26 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
         nmax = std::max(nmax, n_nodes[i]);
         T += n_nodes[i];
     }
-    int tiles = 1;
-    while (tiles < SLED_TREE_TILES && 16 * tiles < G * nmax) tiles *= 2;
-    std::vector<int> groups(B);
-    for (int i = 0; i < B; i++) groups[i] = ceil_div(G * n_nodes[i], 16 * tiles);
-    const int tgt = m->batch_invariant ? SLED_FIXED_CHUNK_PAGES : tree_pages_per_item(np, groups, Hkv);
-    auto chunk_of = [&](int i) {
-        const int c = m->batch_invariant ? SLED_FIXED_CHUNK_PAGES : attn_chunk(std::max(np[i], 1), tgt);
-        return ceil_div(c, P) * P;   // a step of the kernel is P pages
-    };
-    int64_t n_items = 0, n_mass = 0, mass_chunk = MASS_ITEM_PAGES;
-    while (n_pages * Hkv / mass_chunk > 8192) mass_chunk *= 2;
     for (int i = 0; i < B; i++) {
-        n_items += (int64_t)groups[i] * Hkv * std::max(1, ceil_div(np[i], chunk_of(i)));
-        n_mass += (int64_t)Hkv * ceil_div(ceil_div(p->reqs[req_ids[i]].len_ub + n_nodes[i], 16), (int)mass_chunk);
+        at_group[i] = (int)groups.size();
+        const int all = ceil_div(G * n_nodes[i], 16);
+        for (int t = 0; t < all; t += SLED_TREE_TILES) {
+            const int tiles = std::min(all - t, SLED_TREE_TILES);
+            groups.push_back({i, t, tiles, tree_waves(tiles), np[i]});
+        }
     }
-    const tree_layout w = tree_plan_layout(m, n_items, n_mass, T, n_pages, tiles);
+    at_group[B] = (int)groups.size();
+    const int tgt = m->batch_invariant ? 0 : tree_item_length(groups, Hkv, P);
+    auto chunk_of = [&](const tree_group& x) { return m->batch_invariant ? SLED_FIXED_CHUNK_PAGES : tree_chunk(x, tgt, P); };
+    int64_t n_items = 0, n_slots = 0, n_mass = 0, mass_chunk = MASS_ITEM_PAGES;
+    while (n_pages * Hkv / mass_chunk > 8192) mass_chunk *= 2;
+    for (const tree_group& x : groups) {
+        const int64_t items = (int64_t)Hkv * std::max(1, ceil_div(x.pages, chunk_of(x)));
+        n_items += items;
+        n_slots += items * x.waves;
+    }
+    for (int i = 0; i < B; i++) n_mass += (int64_t)Hkv * ceil_div(ceil_div(p->reqs[req_ids[i]].len_ub + n_nodes[i], 16), (int)mass_chunk);
+    const tree_layout w = tree_plan_layout(m, n_items, n_slots, n_mass, T, n_pages);
     if (w.total > workspace_bytes) SLED_FAIL(SLED_EINVAL, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, w.total);
     sled_stage_slot* sl;
     if ((rc = stage_acquire(p, w.ints / 4, &sl)) != SLED_OK) return rc;
@@ -1420,16 +1437,19 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
         row += n_nodes[i];
     }
     std::stable_sort(by_length.begin(), by_length.end(), [&](int a, int b) { return np[a] > np[b]; });
-    int at = 0;
+    int at = 0, slot = 0;
     for (int i : by_length) {
-        const int chunk = chunk_of(i), runs = std::max(1, ceil_div(np[i], chunk)), first = at, stride = groups[i] * Hkv;
-        for (int c = 0; c < runs; c++)
-            for (int r = 0; r < groups[i]; r++)
+        for (int k = at_group[i]; k < at_group[i + 1]; k++) {
+            const tree_group& x = groups[k];
+            const int chunk = chunk_of(x), runs = std::max(1, ceil_div(np[i], chunk)), first = at;
+            for (int c = 0; c < runs; c++)
                 for (int g = 0; g < Hkv; g++, at++) {
                     const int32_t rec[SLED_TREE_ITEM] = {req_ids[i], g, c * chunk, std::min(chunk, np[i] - c * chunk), n_nodes[i], row0[i], page_at[i],
-                                                         first + r * Hkv + g, runs, stride, r * 16 * tiles, c == runs - 1};
+                                                         first + g, runs, Hkv, x.tile0 * 16, c == runs - 1, x.tiles, x.waves, slot + g * x.waves};
                     memcpy(item + (size_t)at * SLED_TREE_ITEM, rec, sizeof(rec));
                 }
+            slot += runs * Hkv * x.waves;
+        }
         const int all = ceil_div(p->reqs[req_ids[i]].len_ub + n_nodes[i], 16);
         for (int p0 = 0; p0 < all; p0 += (int)mass_chunk)
             for (int g = 0; g < Hkv; g++, mass_item += 8) {
@@ -1450,7 +1470,6 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
     t.part_ml = reinterpret_cast<float*>(ws + w.part_ml);
     t.n_items = (int)n_items;
     t.n_mass_items = (int)n_mass;
-    t.tiles = tiles;
     t.max_nodes = nmax;
     t.T = T;
     // what earlier steps staged for these requests is overwritten, and only the last trees can be committed

@@ -174,10 +174,12 @@ struct sled_request {
 };
 
 // A batch of draft trees, planned by sled_tree_begin: device arrays in the caller's workspace and the sizes of the launches over them
-constexpr int SLED_TREE_TILES = 4;   // row tiles of 16 that an attention work item covers at most
-constexpr int SLED_TREE_ITEM = 12;   // ints of an attention work item:
+constexpr int SLED_TREE_TILES = 8;   // row tiles of 16 that an attention work item covers at most
+constexpr int SLED_TREE_RUN = 1024;  // pages of an attention work item at most
+constexpr int SLED_TREE_ITEM = 16;   // ints of an attention work item:
 //   [0] request id  [1] kv head  [2] first page  [3] pages  [4] nodes  [5] first packed row  [6] first entry of the request's page list
-//   [7] first item of this (request, kv head, row group)  [8] how many there are  [9] how far apart  [10] first stacked row  [11] has the tree
+//   [7] first item of this (request, kv head, row group)  [8] how many there are  [9] how far apart  [10] first stacked row  [11] has the tree  [12] row tiles
+//   [13] wavefronts that share them: 2, 4 or 8  [14] first tile's slot among the partial states of item [7]  [15] unused
 struct sled_tree_plan {
     const int32_t* items;        // [n_items][SLED_TREE_ITEM]
     const int32_t* mass_items;   // [n_mass_items][8]  as [0] .. [6] above
@@ -187,7 +189,6 @@ struct sled_tree_plan {
     float* part_o;               // states of split items
     float* part_ml;
     int n_items, n_mass_items;
-    int tiles;                   // row tiles of 16 that a work item covers: 1, 2 or SLED_TREE_TILES
     int max_nodes, T;
 };
 

@@ -6,22 +6,21 @@
 //   s_t = q_jh . K_gt / sqrt(D)   (t < L, and the nodes t in A(j))
 //   lse = log sum exp(s_t),   out = sum exp(s_t - lse) V_gt
 //
-// tree_attention_kernel, per work item (request, kv head, group of 16 NT stacked rows, run of context pages):
-//   All G heads of all nodes are stacked into tiles of 16 rows (row r = node r / G, head r % G), so that K and V are read once for up to 64
-//   rows.  A workgroup is four wavefronts that share nothing while they read: each takes every fourth pair of pages straight
-//   from memory into its registers, in the operand order that pages are stored in, PFB pairs ahead, and multiplies
-//   it with every row tile.  No barrier and no LDS traffic but the queries' operands stand in the loop.
+// tree_attention_kernel, per work item (request, kv head, group of stacked rows, run of context pages):
+//   All G heads of all nodes are stacked into tiles of 16 rows (row r = node r / G, head r % G), so that K and V are read from memory once for up to
+//   128 rows.  The eight wavefronts of a workgroup, one workgroup a CU, read a step's K and V (32 tokens: two pages) together, 16 bytes a lane, into
+//   registers, 64 KB ahead, and hand them over through LDS in the order the products want them.  Each has one row tile; with no more
+//   than four (two) tiles, two (four) groups of wavefronts take a step each.
 //     S^T[32 tokens, 16 rows] = K Q^T    v_mfma_f32_16x16x32_bf16, page by page
 //     O^T[128 dims, 16 rows] += V^T P^T  the same instruction over both pages at once: a lane holds, of S^T, the four tokens of its
 //                                        quad in each page, and these eight are its part of the operand P^T, as the quads of V are of V^T
-//   p = 2^(s' - M), s' in log2 units, M a whole number that a row raises when some s' passes it by more than 8; every rescale is then an
+//   p = 2^(s' - M), s' in log2 units, M a whole number that a row raises when some s' passes it by more than 16; every rescale is then an
 //   exact power of two, so neither the order of the pages nor their split over wavefronts changes how p is rounded.  p enters the second product as
 //   a bf16 pair (16 bits), which costs 8 of 24 instructions: with a single bf16 the error would be that of the output's own
 //   rounding once more.  Sums are float32.
-//   The tree's own keys and values come from the caller's k and v through an LDS image in page order, as one or two more steps under the
-//   ancestors' bits; the item that reads them also writes them into the request's tail slots, which nobody reads in this launch.
-//   The wavefronts' states are added up through LDS; the items of a (request, kv head, row group) store theirs and the last to arrive adds
-//   them up in ascending order.
+//   The tree's own keys and values come from the caller's k and v as one or two more steps under the ancestors' bits; the item that reads them also
+//   writes them into the request's tail slots, which nobody reads in this launch.  Items of one (request, kv head, row group) store their
+//   states and the last to arrive adds them up in ascending order.
 //   fp32 models: the same with v_mfma_f32_16x16x4_f32 and single pages.
 // A value that is not finite must not reach the rows that do not see its node (0 * inf is NaN): such values of v are left out of the
 // product and added at the end for the rows that do see them.  Slots of the last context page behind L count as zero.
@@ -32,10 +31,11 @@
 namespace {
 
 constexpr float NEG_BIG = -1.0e30f;
-constexpr int WAVES = 4;
+constexpr int WAVES = 8;
 
 // (vectors of the compiler's own: structs of four would not stay in registers where their parts are used)
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // sizes of one step of the page loop
@@ -44,59 +44,103 @@ struct Geo {
     static constexpr int P = F32 ? 1 : 2;        // pages
     static constexpr int TOK = 16 * P;           // tokens
     static constexpr int DT = D / 16;            // tiles of 16 dims of an output
-    static constexpr int OWN = DT / WAVES;       // of them, the ones a wavefront adds up at the end
     static constexpr int QC = F32 ? D / 16 : 4;  // operand pieces (16 bytes a lane) of a row tile, per plane
     static constexpr int ELEM = F32 ? 4 : 2;
+    static constexpr int CH = D * ELEM / 16;     // 16-byte pieces of a token
+    static constexpr int BYTES = TOK * D * ELEM; // of K or of V
+    static constexpr int LOADS = 2 * BYTES / (64 * WAVES * 16);   // pieces that a thread moves: one of K and one of V, or (1) the upper half of the threads V
 };
 
-// one step's K and V as the lanes hold them
+// one step's K, and its V with the weights it is to be multiplied by, as the lanes hold them
 template <int D, bool F32>
-struct KV {
+struct Keys {
     u32x4 k[2][4];   // [page][32 dims]: token lane % 16, dims (lane / 16) * 8 ..
-    u32x4 v[2][4];   // [page][32 dims]: tokens (lane / 16) * 4 .. + 3 of dim lane % 16, then of dim lane % 16 + 16
 };
 template <int D>
-struct KV<D, true> {
-    f32x4 k[D / 16];      // token lane % 16, dims 16 c + (lane / 16) * 4 ..
+struct Keys<D, true> {
+    f32x4 k[D / 16];   // token lane % 16, dims 16 c + (lane / 16) * 4 ..
+};
+template <int D, bool F32>
+struct Values {
+    u32x4 v[8];      // [16 dims]: tokens (lane / 16) * 4 .. + 3 of dim lane % 16, of the first page and of the second
+    u32x4 hi, lo;    // weights of these tokens for row lane % 16
+};
+template <int D>
+struct Values<D, true> {
     float v[D / 16][4];   // token (lane / 16) * 4 + i, dim 16 dt + lane % 16
+    float w[4];
 };
 
+// A step in LDS: K, then V.  bf16: K pages as they are in the pool, V as the operands of its eight tiles of dims.  fp32: K as [16 dims][lane] pieces
+// of 16 bytes, V as rows whose runs of 16 dims are turned by token / 4 places within their four: lane groups read tokens four
+// apart and so meet different banks.
+__device__ __forceinline__ int turned(int t, int q) { return (q & ~15) | ((q + (t >> 2) * 4) & 12) | (q & 3); }
+
 template <int D, bool F32>
-__device__ __forceinline__ void load_page(KV<D, F32>& kv, int sub, const void* kp, const void* vp, int lane) {
+__device__ __forceinline__ void read_keys(Keys<D, F32>& kv, const char* step, int lane) {
+    const u32x4* k = reinterpret_cast<const u32x4*>(step) + lane;
     if constexpr (!F32) {
 #pragma unroll
-        for (int c = 0; c < 4; c++) kv.k[sub][c] = reinterpret_cast<const u32x4*>(kp)[c * 64 + lane];
+        for (int p = 0; p < 2; p++)
 #pragma unroll
-        for (int c = 0; c < 4; c++) kv.v[sub][c] = reinterpret_cast<const u32x4*>(vp)[c * 64 + lane];
+            for (int c = 0; c < 4; c++) kv.k[p][c] = k[p * 256 + c * 64];
     } else {
-        const float* k = static_cast<const float*>(kp) + (lane & 15) * D + (lane >> 4) * 4;
-        const float* v = static_cast<const float*>(vp) + (lane >> 4) * 4 * D + (lane & 15);
 #pragma unroll
-        for (int c = 0; c < D / 16; c++) kv.k[c] = *reinterpret_cast<const f32x4*>(k + 16 * c);
+        for (int c = 0; c < D / 16; c++) kv.k[c] = __builtin_bit_cast(f32x4, k[c * 64]);
+    }
+}
+template <int D, bool F32>
+__device__ __forceinline__ void read_values(Values<D, F32>& kv, const char* step, int lane) {
+    if constexpr (!F32) {
+        const u32x4* v = reinterpret_cast<const u32x4*>(step + Geo<D, F32>::BYTES) + lane;
+#pragma unroll
+        for (int dt = 0; dt < 8; dt++) kv.v[dt] = v[dt * 64];
+    } else {
+        const float* v = reinterpret_cast<const float*>(step + Geo<D, F32>::BYTES) + (lane >> 4) * 4 * D + (lane & 15);
 #pragma unroll
         for (int dt = 0; dt < D / 16; dt++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) kv.v[dt][i] = v[i * D + dt * 16];
+            for (int i = 0; i < 4; i++) kv.v[dt][i] = v[i * D + ((dt & ~3) | ((dt + (lane >> 4)) & 3)) * 16];
     }
 }
 
-// values of tokens lim .. of the step become zero
+// this thread's share of a step on its way to LDS
 template <int D, bool F32>
-__device__ __forceinline__ void cut_values(KV<D, F32>& kv, int lim, int lane) {
-    const int t0 = (lane >> 4) * 4;
-    if constexpr (!F32) {
-#pragma unroll
-        for (int p = 0; p < 2; p++) {
-            const int t = p * 16 + t0;
-            const uint32_t a = (t < lim ? 0xffffu : 0u) | (t + 1 < lim ? 0xffff0000u : 0u), b = (t + 2 < lim ? 0xffffu : 0u) | (t + 3 < lim ? 0xffff0000u : 0u);
-#pragma unroll
-            for (int c = 0; c < 4; c++) kv.v[p][c] &= u32x4{a, b, a, b};
-        }
+struct Cargo {
+    u32x4 x[Geo<D, F32>::LOADS];
+};
+template <int D, bool F32>
+__device__ __forceinline__ bool is_value(int u, int wave) {
+    return Geo<D, F32>::LOADS == 2 ? u == 1 : wave >= WAVES / 2;
+}
+
+// values of tokens lim .. count as zero; e: the piece's number among those of V
+template <int D, bool F32>
+__device__ __forceinline__ void cut_values(u32x4& x, int lim, int e) {
+    if constexpr (F32) {
+        if (e / Geo<D, F32>::CH >= lim) x = u32x4{0u, 0u, 0u, 0u};
     } else {
-#pragma unroll
-        for (int dt = 0; dt < D / 16; dt++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) kv.v[dt][i] = t0 + i < lim ? kv.v[dt][i] : 0.f;
+        const int t = (e >> 8) * 16 + ((e >> 4) & 3) * 4;   // the piece holds tokens t .. t + 3 of two dims
+        const uint32_t a = (t < lim ? 0xffffu : 0u) | (t + 1 < lim ? 0xffff0000u : 0u), b = (t + 2 < lim ? 0xffffu : 0u) | (t + 3 < lim ? 0xffff0000u : 0u);
+        x &= u32x4{a, b, a, b};
+    }
+}
+
+// piece e of K or V of context pages
+template <int D, bool F32>
+__device__ __forceinline__ void store_piece(const u32x4& x, bool value, int e, char* step) {
+    constexpr int CH = Geo<D, F32>::CH;
+    if constexpr (F32) {
+        const int t = e / CH, q = e % CH;
+        if (value) reinterpret_cast<u32x4*>(step + Geo<D, F32>::BYTES)[t * CH + turned(t, q)] = x;
+        else reinterpret_cast<u32x4*>(step)[(q >> 2) * 64 + (q & 3) * 16 + t] = x;
+    } else if (value) {
+        // 8 bytes of each of two operands
+        u32x2* v = reinterpret_cast<u32x2*>(step + 8192) + (((e & 255) >> 6) * 128 + (e & 63)) * 2 + (e >> 8);
+        v[0] = u32x2{x[0], x[1]};
+        v[128] = u32x2{x[2], x[3]};
+    } else {
+        reinterpret_cast<u32x4*>(step)[e] = x;
     }
 }
 
@@ -113,27 +157,22 @@ __device__ __forceinline__ float sum_over_groups(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// S^T of one page (A operand K, B operand Q) or, SWAP, S (A operand Q, B operand K) of a row tile
-template <int D, bool F32, int PL, bool SWAP>
-__device__ __forceinline__ float4_t page_scores(const KV<D, F32>& kv, int sub, const u32x4* q /* the tile's operand pieces + lane */) {
+// S of a row tile against one page (A operand Q, B operand K)
+template <int D, bool F32, int PL>
+__device__ __forceinline__ float4_t page_scores(const Keys<D, F32>& kv, int sub, const u32x4* q /* the tile's operand pieces + lane */) {
     float4_t s = {0.f, 0.f, 0.f, 0.f};
     if constexpr (!F32) {
 #pragma unroll
-        for (int ks = 0; ks < 4; ks++) {
-            const bf16x8_t k = __builtin_bit_cast(bf16x8_t, kv.k[sub][ks]);
+        for (int ks = 0; ks < 4; ks++)
 #pragma unroll
-            for (int pl = 0; pl < PL; pl++) {
-                const bf16x8_t x = __builtin_bit_cast(bf16x8_t, q[(pl * 4 + ks) * 64]);
-                s = SWAP ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, k, s, 0, 0, 0) : __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, x, s, 0, 0, 0);
-            }
-        }
+            for (int pl = 0; pl < PL; pl++)
+                s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, q[(pl * 4 + ks) * 64]), __builtin_bit_cast(bf16x8_t, kv.k[sub][ks]), s, 0, 0, 0);
     } else {
 #pragma unroll
         for (int c = 0; c < D / 16; c++) {
             const f32x4 kk = kv.k[c], xx = __builtin_bit_cast(f32x4, q[c * 64]);
 #pragma unroll
-            for (int e = 0; e < 4; e++)
-                s = SWAP ? __builtin_amdgcn_mfma_f32_16x16x4f32(xx[e], kk[e], s, 0, 0, 0) : __builtin_amdgcn_mfma_f32_16x16x4f32(kk[e], xx[e], s, 0, 0, 0);
+            for (int e = 0; e < 4; e++) s = __builtin_amdgcn_mfma_f32_16x16x4f32(xx[e], kk[e], s, 0, 0, 0);
         }
     }
     return s;
@@ -177,392 +216,501 @@ __device__ __forceinline__ void stage_queries(u32x4* qs, const tree_args& a, int
     }
 }
 
-// The running state of a wavefront: row lane % 16 of every tile, dims 16 dt + (lane / 16) * 4 + e
-template <int NT, int DT>
+// The running state of a wavefront: row lane % 16 of its tile, dims 16 dt + (lane / 16) * 4 + e
+template <int DT>
 struct State {
-    float m[NT], l[NT];
-    float4_t o[NT][DT];
+    float m, l;   // reference; this lane's part of the sum
+    float4_t o[DT];
 };
 
-// One step (16 P tokens) against the first n_tiles row tiles.  MASKED: bit t of bits[tile] says whether this lane's row sees token t.
-template <int NT, int D, bool F32, int PL, bool MASKED>
-__device__ __forceinline__ void tile_steps(const KV<D, F32>& kv, const u32x4* qs, int lane, int n_tiles, float c, const uint32_t* bits, State<NT, D / 16>& st) {
-    constexpr int P = Geo<D, F32>::P, DT = Geo<D, F32>::DT, QT = Geo<D, F32>::QC * 64 * PL;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Scores of a step against the wavefront's row tile, their weights, and V on its way.  MASKED: bit t of `bits` says whether this lane's row sees token t.
+template <int D, bool F32, int PL, bool MASKED>
+__device__ __forceinline__ void weigh(const char* step, const u32x4* q, int lane, float c, uint32_t bits, State<D / 16>& st, Values<D, F32>& x_v) {
+    constexpr int P = Geo<D, F32>::P, DT = Geo<D, F32>::DT;
     const int t0 = (lane >> 4) * 4;
-    if (NT >= 4) asm volatile("" ::: "memory");   // the queries' operands are read again in every step: there are not registers for all
+    Keys<D, F32> kv;
+    read_keys<D, F32>(kv, step, lane);
+    read_values<D, F32>(x_v, step, lane);
+    __builtin_amdgcn_sched_barrier(0);   // (V is on its way while the scores are made)
+    float4_t s[P];
 #pragma unroll
-    for (int t = 0; t < NT; t++) {
-        if (t >= n_tiles) break;
-        float4_t s[P];
+    for (int p = 0; p < P; p++) s[p] = float4_t{0.f, 0.f, 0.f, 0.f};
+    if constexpr (!F32) {
 #pragma unroll
-        for (int p = 0; p < P; p++) s[p] = page_scores<D, F32, PL, false>(kv, p, qs + t * QT + lane);
-        if (MASKED) {
+        for (int ks = 0; ks < 4; ks++)
 #pragma unroll
-            for (int p = 0; p < P; p++)
+            for (int pl = 0; pl < PL; pl++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) s[p][i] = (bits[t] >> (p * 16 + t0 + i)) & 1u ? s[p][i] : -INFINITY;
+                for (int p = 0; p < P; p++)
+                    s[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv.k[p][ks]), __builtin_bit_cast(bf16x8_t, q[pl * 4 + ks]), s[p], 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int d = 0; d < D / 16; d++) {
+            const f32x4 kk = kv.k[d], xx = __builtin_bit_cast(f32x4, q[d]);
+#pragma unroll
+            for (int e = 0; e < 4; e++) s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[e], xx[e], s[0], 0, 0, 0);
         }
-        float x[P][4], top = -INFINITY;
+    }
+    if (MASKED) {
 #pragma unroll
         for (int p = 0; p < P; p++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                x[p][i] = fmaf(s[p][i], c, -st.m[t]);
-                top = fmaxf(top, x[p][i]);
-            }
-        if (__builtin_amdgcn_ballot_w64(top > 8.f) != 0ull) {
-            // some row's reference is too low: raise it to a whole number (row by row; the four lanes of a row agree)
-            float hi = s[0][0];
+            for (int i = 0; i < 4; i++) s[p][i] = (bits >> (p * 16 + t0 + i)) & 1u ? s[p][i] : -INFINITY;
+    }
+    float x[P * 4], top = -INFINITY;
 #pragma unroll
-            for (int p = 0; p < P; p++)
+    for (int p = 0; p < P; p++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) hi = fmaxf(hi, s[p][i]);
-            const float mnew = fmaxf(st.m[t], ceilf(max_over_groups(hi) * c));
-            const float alpha = __builtin_amdgcn_exp2f(st.m[t] - mnew);
-            st.m[t] = mnew;
-            st.l[t] *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) st.o[t][dt][e] *= alpha;
-#pragma unroll
-            for (int p = 0; p < P; p++)
-#pragma unroll
-                for (int i = 0; i < 4; i++) x[p][i] = fmaf(s[p][i], c, -mnew);
+        for (int i = 0; i < 4; i++) {
+            x[p * 4 + i] = fmaf(s[p][i], c, -st.m);
+            top = fmaxf(top, x[p * 4 + i]);
         }
-        float ps = 0.f;
-        if constexpr (!F32) {
-            bf16x8_t ph, pl;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > 16.f) != 0ull, 0)) {
+        // some row's reference is too low: raise it to a whole number (row by row; the four lanes of a row agree)
+        float hi = s[0][0];
 #pragma unroll
-            for (int p = 0; p < 2; p++)
+        for (int i = 1; i < P * 4; i++) hi = fmaxf(hi, s[i >> 2][i & 3]);
+        const float mnew = fmaxf(st.m, ceilf(max_over_groups(hi) * c)), alpha = __builtin_amdgcn_exp2f(st.m - mnew);
+        st.m = mnew;
+        st.l *= alpha;
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const float w = __builtin_amdgcn_exp2f(x[p][i]);
-                    ps += w;
-                    const __bf16 h = (__bf16)w;   // to nearest even
-                    ph[p * 4 + i] = h;
-                    pl[p * 4 + i] = (__bf16)(w - (float)h);
-                }
+        for (int dt = 0; dt < DT; dt++)
 #pragma unroll
-            for (int dt = 0; dt < DT; dt++) {
-                const u32x4 a = kv.v[0][dt >> 1], b = kv.v[1][dt >> 1];
-                const bf16x8_t va = __builtin_bit_cast(bf16x8_t, (dt & 1) ? __builtin_shufflevector(a, b, 2, 3, 6, 7) : __builtin_shufflevector(a, b, 0, 1, 4, 5));
-                st.o[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, ph, st.o[t][dt], 0, 0, 0);
-                st.o[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl, st.o[t][dt], 0, 0, 0);
-            }
-        } else {
-            float w[4];
+            for (int e = 0; e < 4; e++) st.o[dt][e] *= alpha;
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                w[i] = __builtin_amdgcn_exp2f(x[0][i]);
-                ps += w[i];
-            }
+        for (int i = 0; i < P * 4; i++) x[i] = fmaf(s[i >> 2][i & 3], c, -st.m);
+    }
+    float w[P * 4];
 #pragma unroll
-            for (int dt = 0; dt < DT; dt++)
+    for (int i = 0; i < P * 4; i++) w[i] = __builtin_amdgcn_exp2f(x[i]);
+    if constexpr (!F32) {
 #pragma unroll
-                for (int i = 0; i < 4; i++) st.o[t][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv.v[dt][i], w[i], st.o[t][dt], 0, 0, 0);
+        for (int i = 0; i < 4; i++) {
+            x_v.hi[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{w[2 * i], w[2 * i + 1]}), bf16x2));   // to nearest even
+            const float r0 = w[2 * i] - __uint_as_float(x_v.hi[i] << 16), r1 = w[2 * i + 1] - __uint_as_float(x_v.hi[i] & 0xffff0000u);
+            x_v.lo[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{r0, r1}), bf16x2));
         }
-        st.l[t] += ps;
+        st.l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) x_v.w[i] = w[i];
+        st.l += (w[0] + w[1]) + (w[2] + w[3]);
+    }
+}
+
+template <int D, bool F32>
+__device__ __forceinline__ void gather(const Values<D, F32>& x, State<D / 16>& st) {
+    constexpr int DT = D / 16;
+    if constexpr (!F32) {
+        const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, x.hi), pl = __builtin_bit_cast(bf16x8_t, x.lo);
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x.v[dt]), ph, st.o[dt], 0, 0, 0);
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x.v[dt]), pl, st.o[dt], 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.v[dt][i], x.w[i], st.o[dt], 0, 0, 0);
     }
 }
 
 __device__ __forceinline__ bool not_finite(bf16_t x) { return (x & 0x7f80) == 0x7f80; }
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
-constexpr int PFB = 2;   // steps whose pages are in registers or on their way
+// of 16 bytes of values: whether one of them is not finite (an exponent of ones), and the others alone
+template <bool F32>
+__device__ __forceinline__ bool has_not_finite(const u32x4& v) {
+    constexpr uint32_t EXP = F32 ? 0x7f800000u : 0x7f807f80u, ONE = F32 ? 0x00800000u : 0x00800080u, TOP = F32 ? 0x80000000u : 0x80008000u;
+    uint32_t over = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; i++) over |= (v[i] & EXP) + ONE;   // the exponent of ones carries into the sign's place
+    return (over & TOP) != 0u;
+}
+template <bool F32>
+__device__ __forceinline__ u32x4 finite_only(u32x4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if constexpr (F32) {
+            if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] = 0u;
+        } else {
+            if ((v[i] & 0x7f80u) == 0x7f80u) v[i] &= 0xffff0000u;
+            if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0xffffu;
+        }
+    }
+    return v;
+}
 
-// bytes of LDS: the queries' operands and the image of the tree's keys and values; afterwards the states of up to two row tiles
-template <int NT, int D, bool F32, int PL>
+// register i of lane group g <-> register g of lane group i
+__device__ __forceinline__ void quad_transpose(u32x4& v) {
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const auto x = __builtin_amdgcn_permlane32_swap(v[i], v[i + 2], false, false);
+        v[i] = x[0];
+        v[i + 2] = x[1];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const auto x = __builtin_amdgcn_permlane16_swap(v[i], v[i + 1], false, false);
+        v[i] = x[0];
+        v[i + 1] = x[1];
+    }
+}
+
+// bytes of LDS: two steps of every token group; afterwards the states that the token groups exchange
+template <int NR, int D, bool F32>
 constexpr size_t attention_lds() {
-    constexpr size_t loop = (size_t)NT * 16 * PL * D * Geo<D, F32>::ELEM + (size_t)2 * SLED_TREE_MAX * D * Geo<D, F32>::ELEM;
-    constexpr size_t merge = (size_t)(NT < 2 ? NT : 2) * WAVES * Geo<D, F32>::DT * 256 * sizeof(float);
+    constexpr size_t NG = WAVES / NR, loop = 2 * NG * 2 * Geo<D, F32>::BYTES, merge = NG > 1 ? (size_t)WAVES * Geo<D, F32>::DT * 1024 : 0;
     return loop > merge ? loop : merge;
 }
 
-template <int NT, int D, bool F32, bool STEP>
-__global__ __launch_bounds__(64 * WAVES, 1) void tree_attention_kernel(tree_args a) {
+// LDS beside the steps
+struct tree_shared {
+    int pages[SLED_TREE_RUN];
+    float m[WAVES * 16], l[WAVES * 16];   // [token group][row]
+    uint32_t bad[2];                      // nodes with values that are not finite
+    int last;
+};
+
+// NR wavefronts share the row tiles (one each), WAVES / NR groups of wavefronts share the steps
+template <int NR, int D, bool F32, bool STEP>
+__device__ __forceinline__ void attend_item(const tree_args& a, const int32_t* rec, unsigned char* smem, tree_shared& sh) {
     using G_ = Geo<D, F32>;
     using T = std::conditional_t<F32, float, bf16_t>;
-    constexpr int P = G_::P, TOK = G_::TOK, DT = G_::DT, OWN = G_::OWN, PL = STEP && !F32 ? 2 : 1, ROWS = NT * 16;
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    __shared__ float sh_m[WAVES][ROWS], sh_l[WAVES][ROWS];
-    __shared__ uint32_t sh_bad[2];
-    __shared__ int sh_last;
-
+    constexpr int NG = WAVES / NR, ROWS = NR * 16, DEPTH = 4 / NG;   // token groups; turns asked for ahead
+    constexpr int P = G_::P, TOK = G_::TOK, DT = G_::DT, OWN = DT / NG, PL = STEP && !F32 ? 2 : 1, LOADS = G_::LOADS, CH = G_::CH, E = 16 / G_::ELEM;
     const int w = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int32_t* rec = a.t.items + SLED_TREE_ITEM * w;
     const int req = rec[0], g = rec[1], page0 = rec[2], npg = rec[3], n = rec[4], row0 = rec[5], w0 = rec[7], n_items = rec[8], stride = rec[9], r0 = rec[10];
     const bool last = rec[11] != 0;   // the item that has the tree
+    const int n_tiles = rec[12], slot0 = rec[14];
     const int32_t* pages = a.t.pages + rec[6];
+    for (int i = tid; i < max(npg, 1); i += 64 * WAVES) sh.pages[i] = pages[page0 + i];   // (without context: the tail's page)
     const int L = a.len_dev[req];
     const int G = a.Hq / a.Hkv, rows = G * n;
-    const int n_tiles = min(NT, (rows - r0 + 15) >> 4);
-    const int lr = lane & 15, lg = lane >> 4;
-
-    // this wavefront's pages, in steps of P: the item's, as far as there is context
-    const int page_end = min(page0 + npg, (L + 15) >> 4);
-    const int n_steps_all = page_end > page0 ? (page_end - page0 + P - 1) / P : 0;
-    const int n_steps = n_steps_all > wave ? (n_steps_all - wave + WAVES - 1) / WAVES : 0;
-    constexpr int BLK = 64 / P;   // steps whose page numbers the lanes hold
-    auto page_ids = [&](int it0) {
-        const int i = page0 + ((it0 + lane / P) * WAVES + wave) * P + lane % P;
-        return pages[min(i, max(page_end - 1, 0))];
-    };
+    const int rw = wave % NR, tg = wave / NR, lr = lane & 15, lg = lane >> 4;
+    const bool mine = rw < n_tiles;   // this wavefront has a tile
     const size_t head = (size_t)16 * D, layer_page = (size_t)a.layer * a.n_pages;
-    int ids = 0, ids_next = 0;
-    if (n_steps > 0) ids = page_ids(0);
-    if (n_steps > BLK) ids_next = page_ids(BLK);
-    KV<D, F32> kv[PFB];
-    auto issue = [&](KV<D, F32>& dst, int it) {   // called with it = 0, 1, 2, ..
-        if (it != 0 && it % BLK == 0) {
-            ids = ids_next;
-            if (it + BLK < n_steps) ids_next = page_ids(it + BLK);
-        }
+
+    // the item's steps: its pages, as far as there is context, then the tree's
+    const int n_pages = max(0, min(npg, ((L + 15) >> 4) - page0)), n_ctx = (n_pages + P - 1) / P;
+    const int n_sub = n_ctx + (last ? (n + TOK - 1) / TOK : 0), n_turns = (n_sub + NG - 1) / NG;
+    const int n_full = max(0, min(L - page0 * 16, n_pages * 16)) / TOK / (NG * DEPTH) * DEPTH;   // turns, in rounds of DEPTH, without a mask
+    if (tid < 2) sh.bad[tid] = 0u;
+    __syncthreads();
+
+    // Turns on their way, DEPTH of them.  Every request is made, whatever the turn: one behind the last step asks for one line again.  So the number
+    // of requests behind the one that is waited for is always the same, and nothing else has to be waited for.
+    Cargo<D, F32> cargo[DEPTH][NG];
+    const int half = (F32 ? 0 : wave >> 2);   // which of the step's pages this wavefront's pieces belong to
+    const int e = LOADS == 2 ? tid : tid & (32 * WAVES - 1);   // the thread's piece of K or V
+    const char* k_base = static_cast<const char*>(a.k_pool) + (layer_page * a.Hkv + g) * head * G_::ELEM;
+    const char* v_base = static_cast<const char*>(a.v_pool) + (layer_page * a.Hkv + g) * head * G_::ELEM;
+    const uint32_t page_bytes = (uint32_t)(a.Hkv * head * G_::ELEM), lane_off = (F32 ? e : tid & 255) * 16;
+    int ids[NG];   // pages of the next request: read from LDS a turn before they are needed
+    auto next_ids = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int phys = __builtin_amdgcn_readlane(ids, it % BLK * P + p);
-            const size_t at = ((layer_page + phys) * a.Hkv + g) * head;
-            load_page<D, F32>(dst, p, static_cast<const T*>(a.k_pool) + at, static_cast<const T*>(a.v_pool) + at, lane);
+        for (int u = 0; u < NG; u++) ids[u] = sh.pages[max(0, min(P * (s * NG + u) + half, n_pages - 1))];   // (any page that there is)
+    };
+    auto load = [&](Cargo<D, F32>* to, int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < NG; u++) {
+            const int i = s * NG + u;
+            const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(ids[u]) * page_bytes;
+            if (i < n_ctx || i >= n_sub) {
+#pragma unroll
+                for (int x = 0; x < LOADS; x++) to[u].x[x] = *reinterpret_cast<const u32x4*>((is_value<D, F32>(x, wave) ? v_base : k_base) + at + lane_off);
+            } else {
+                const size_t j = row0 + min((i - n_ctx) * TOK + e / CH, n - 1);
+#pragma unroll
+                for (int x = 0; x < LOADS; x++) {
+                    const bool value = is_value<D, F32>(x, wave);
+                    to[u].x[x] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(value ? a.v : a.k) + (j * (value ? a.v_stride : a.k_stride) + g * D) * G_::ELEM + e % CH * 16);
+                }
+            }
+        }
+        asm volatile("" ::: "memory");   // asked for here, not where it is needed
+        next_ids(s + 1);
+    };
+    auto step_at = [&](int s, int u) __attribute__((always_inline)) { return reinterpret_cast<char*>(smem) + ((s & 1) * NG + u) * 2 * G_::BYTES; };
+    auto store = [&](Cargo<D, F32>* from, int s, auto masked) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < NG; u++) {
+            const int i = s * NG + u;
+            char* to = step_at(s, u);
+            if (!masked || i < n_ctx) {
+                const int lim = L - (page0 + i * P) * 16;   // context tokens from the step's first on
+#pragma unroll
+                for (int x = 0; x < LOADS; x++) {
+                    const bool value = is_value<D, F32>(x, wave);
+                    if (masked && value && lim < TOK) cut_values<D, F32>(from[u].x[x], lim, e);
+                    store_piece<D, F32>(from[u].x[x], value, e, to);
+                }
+            } else if (i < n_sub) {
+                // nodes: rows of the caller's, their values turned here
+#pragma unroll
+                for (int x = 0; x < LOADS; x++) {
+                    const bool value = is_value<D, F32>(x, wave);
+                    const int t = e / CH, c = e % CH, j = (i - n_ctx) * TOK + t;
+                    if (!value) {
+                        if constexpr (F32) reinterpret_cast<u32x4*>(to)[(c >> 2) * 64 + (c & 3) * 16 + t] = from[u].x[x];
+                        else *reinterpret_cast<u32x4*>(to + (t >> 4) * 4096 + kpage_offset(t & 15, c * 8) * 2) = from[u].x[x];
+                        continue;
+                    }
+                    u32x4 v = from[u].x[x];
+                    if (has_not_finite<F32>(v)) {
+                        if (j < n) atomicOr(&sh.bad[j >> 5], 1u << (j & 31));
+                        v = finite_only<F32>(v);
+                    }
+                    // (nodes behind the last repeat it: finite, and their weights are zero)
+                    if constexpr (F32) {
+                        reinterpret_cast<u32x4*>(to + G_::BYTES)[t * CH + turned(t, c)] = v;
+                    } else {
+                        // The wavefront has a token quad: lane group x token x, two dims a register.  Turned about its diagonal, a lane group has two
+                        // dims of every token.
+                        quad_transpose(v);
+                        const int d = c * 8 + lg * 2;
+                        u32x2* dst = reinterpret_cast<u32x2*>(to + G_::BYTES) + ((d >> 4) * 64 + ((t & 15) >> 2) * 16 + (d & 15)) * 2 + (t >> 4);
+                        dst[0] = u32x2{(v[0] & 0xffffu) | (v[1] << 16), (v[2] & 0xffffu) | (v[3] << 16)};
+                        dst[2] = u32x2{(v[0] >> 16) | (v[1] & 0xffff0000u), (v[2] >> 16) | (v[3] & 0xffff0000u)};
+                    }
+                }
+            }
         }
     };
-#pragma unroll
-    for (int u = 0; u < PFB; u++)
-        if (u < n_steps) issue(kv[u], u);
 
-    // queries, and the tree's keys and values, to LDS
-    u32x4* qs = reinterpret_cast<u32x4*>(smem);
-    T* kt = reinterpret_cast<T*>(smem + (size_t)ROWS * PL * D * G_::ELEM);
-    T* vt = kt + (size_t)SLED_TREE_MAX * D;
-    if (tid < 2) sh_bad[tid] = 0u;
-    stage_queries<D, F32, PL>(qs, a, row0, g, G, r0, n_tiles * 16, rows, tid, 64 * WAVES);
-    __syncthreads();
-    if (last) {
-        constexpr int E = 16 / G_::ELEM, CH = D / E;   // elements of 16 bytes, pieces of a row
-        const int filled = (n + TOK - 1) / TOK * TOK;
-        for (int e = tid; e < filled * CH; e += 64 * WAVES) {
-            const int j = e / CH, d = e % CH * E;
-            union {
-                uint4 u;
-                T x[E];
-            } kk, vv;
-            kk.u = vv.u = make_uint4(0u, 0u, 0u, 0u);
-            if (j < n) {
-                kk.u = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.k) + (size_t)(row0 + j) * a.k_stride + g * D + d);
-                vv.u = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.v) + (size_t)(row0 + j) * a.v_stride + g * D + d);
-                if (r0 == 0) {   // into the request's tail slots
-                    const int pos = L + j;
-                    const size_t at = ((layer_page + pages[pos >> 4]) * a.Hkv + g) * head;
-                    T *kp = static_cast<T*>(a.k_pool) + at, *vp = static_cast<T*>(a.v_pool) + at;
-                    if constexpr (F32) {
-                        *reinterpret_cast<uint4*>(kp + (pos & 15) * D + d) = kk.u;
-                        *reinterpret_cast<uint4*>(vp + (pos & 15) * D + d) = vv.u;
-                    } else {
-                        *reinterpret_cast<uint4*>(kp + kpage_offset(pos & 15, d)) = kk.u;
+    // queries, in operand order: row lr of the wavefront's tile, 16 bytes number c
+    u32x4 q[G_::QC * PL];
+    const int r = r0 + rw * 16 + lr, node = mine ? r / G : n;   // this lane's row's node; n and beyond: none
+    const int hh = r - r / G * G;
 #pragma unroll
-                        for (int i = 0; i < E; i++) vp[vpage_offset(pos & 15, d + i)] = vv.x[i];
-                    }
-                }
-                bool bad = false;
+    for (int c = 0; c < G_::QC * PL; c++) {
+        q[c] = u32x4{0u, 0u, 0u, 0u};
+        if (node < n)
+            q[c] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) +
+                                                      ((c / G_::QC) * a.q_plane + (size_t)(row0 + node) * a.q_stride + (size_t)(g * G + hh) * D) * G_::ELEM +
+                                                      (c % G_::QC * 4 + lg) * 16);
+    }
+    const uint64_t seen = node < n ? a.t.seen[row0 + node] : 0ull;
+    next_ids(0);
 #pragma unroll
-                for (int i = 0; i < E; i++)
-                    if (not_finite(vv.x[i])) {
-                        bad = true;
-                        vv.x[i] = 0;
-                    }
-                if (bad) atomicOr(&sh_bad[j >> 5], 1u << (j & 31));
+    for (int u = 0; u < DEPTH; u++) load(cargo[u], u);
+
+    State<DT> st;
+    st.m = NEG_BIG;
+    st.l = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++) st.o[dt] = float4_t{0.f, 0.f, 0.f, 0.f};
+    // The two wavefronts of a SIMD take turns: the upper four make their second product while the lower four make their scores, so that one's
+    // matrix instructions run beside the other's exponentials.  (Wavefronts without a tile work on zeros: they would only wait otherwise.)
+    Values<D, F32> held{};
+    const bool late = wave >= WAVES / 2;
+    auto turn = [&](Cargo<D, F32>* next, int s, auto masked) __attribute__((always_inline)) {
+        // Into the buffer that everybody has read two turns ago; then the next request.  (A barrier for LDS alone: __syncthreads would
+        // wait for the requests too.)
+        store(next, s, masked);
+        if (!masked || s + DEPTH < n_turns) load(next, s + DEPTH);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const int i = s * NG + tg;
+        const char* step = step_at(s, tg);
+        if (late) gather<D, F32>(held, st);
+        if constexpr (!masked) {
+            weigh<D, F32, PL, false>(step, q, lane, a.scale_log2, 0u, st, held);
+        } else if (i < n_sub) {
+            const int lim = L - (page0 + i * P) * 16;
+            const uint32_t bits = i >= n_ctx ? (uint32_t)(seen >> ((i - n_ctx) * TOK)) : lim >= TOK ? ~0u : (1u << lim) - 1u;
+            weigh<D, F32, PL, true>(step, q, lane, a.scale_log2, bits, st, held);
+        } else {
+            held = Values<D, F32>{};
+        }
+        if (!late) gather<D, F32>(held, st);
+    };
+    for (int s = 0; s < n_full; s += DEPTH) {
+#pragma unroll
+        for (int u = 0; u < DEPTH; u++) turn(cargo[u], s + u, std::false_type{});
+    }
+    if (n_full < n_turns)
+        for (int s = n_full;;) {   // (left from the middle)
+            turn(cargo[0], s, std::true_type{});
+            if (++s >= n_turns) break;
+            if constexpr (DEPTH >= 2) {
+                turn(cargo[1], s, std::true_type{});
+                if (++s >= n_turns) break;
             }
-            if constexpr (F32) {
-                *reinterpret_cast<uint4*>(kt + j * D + d) = kk.u;
-                *reinterpret_cast<uint4*>(vt + j * D + d) = vv.u;
-            } else {
-                *reinterpret_cast<uint4*>(kt + (j >> 4) * head + kpage_offset(j & 15, d)) = kk.u;
-#pragma unroll
-                for (int i = 0; i < E; i++) vt[(j >> 4) * head + vpage_offset(j & 15, d + i)] = vv.x[i];
+            if constexpr (DEPTH == 4) {
+                turn(cargo[2], s, std::true_type{});
+                if (++s >= n_turns) break;
+                turn(cargo[3], s, std::true_type{});
+                if (++s >= n_turns) break;
             }
         }
-        __syncthreads();
-    }
+    if (late) gather<D, F32>(held, st);
+    __syncthreads();   // nobody reads a step any more, and sh.bad is complete
 
-    State<NT, DT> st;
+    // sums over the lanes of a row
+    float m = st.m, lsum = sum_over_groups(st.l);
+    float4_t own[OWN];
+    if constexpr (NG == 1) {
 #pragma unroll
-    for (int t = 0; t < NT; t++) {
-        st.m[t] = NEG_BIG;
-        st.l[t] = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < DT; dt++) st.o[t][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
-    }
-    uint32_t bits[NT];
-    // whole steps, PFB - 1 of them in flight behind the one at work; only the last one of the request's last item may be cut by L
-    const int lim = L - (page0 + ((n_steps - 1) * WAVES + wave) * P) * 16;   // context tokens from the last step's first on
-    const int n_whole = n_steps > 0 && lim < TOK ? n_steps - 1 : n_steps;
-    for (int it0 = 0; it0 < n_whole; it0 += PFB) {
-#pragma unroll
-        for (int u = 0; u < PFB; u++) {
-            const int it = it0 + u;
-            if (it < n_whole) {
-                tile_steps<NT, D, F32, PL, false>(kv[u], qs, lane, n_tiles, a.scale_log2, bits, st);
-                if (it + PFB < n_steps) issue(kv[u], it + PFB);
-            }
-        }
-    }
-    if (n_whole < n_steps) {
-        KV<D, F32> cut = kv[0];
-#pragma unroll
-        for (int u = 1; u < PFB; u++)
-            if (n_whole % PFB == u) cut = kv[u];
-        cut_values<D, F32>(cut, lim, lane);
-#pragma unroll
-        for (int t = 0; t < NT; t++) bits[t] = (1u << lim) - 1u;   // (lim is at least 1)
-        kv[0] = cut;
-    }
-    // that step, and the tree's: tokens wave * TOK .. of its nodes
-    const bool tree = last && wave * TOK < n;
-    for (int more = n_whole < n_steps ? 0 : 1; more < (tree ? 2 : 1); more++) {
-        if (more == 1) {
-#pragma unroll
-            for (int p = 0; p < P; p++) load_page<D, F32>(kv[0], p, kt + (wave * P + p) * head, vt + (wave * P + p) * head, lane);
-#pragma unroll
-            for (int t = 0; t < NT; t++) {
-                const int j = (r0 + t * 16 + lr) / G;
-                bits[t] = j < n ? (uint32_t)(a.t.seen[row0 + j] >> (wave * TOK)) : 0u;
-            }
-        }
-        tile_steps<NT, D, F32, PL, true>(kv[0], qs, lane, n_tiles, a.scale_log2, bits, st);
-    }
-    __syncthreads();   // nobody reads the queries or the image any more
-
-    // The wavefronts' states, added up in ascending order: wavefront w takes over the dims of tiles w * OWN ..
-    float4_t own[NT][OWN];
-    float m[NT], lsum[NT];
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-        const float l = sum_over_groups(st.l[t]);
+        for (int i = 0; i < OWN; i++) own[i] = st.o[i];
+    } else {
+        // token groups: each ends up with OWN of the dims' tiles of all of them, added in ascending order
+        float* park = reinterpret_cast<float*>(smem);
         if (lg == 0) {
-            sh_m[wave][t * 16 + lr] = st.m[t];
-            sh_l[wave][t * 16 + lr] = l;
+            sh.m[tg * ROWS + rw * 16 + lr] = m;
+            sh.l[tg * ROWS + rw * 16 + lr] = lsum;
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) *reinterpret_cast<float4_t*>(park + ((wave * DT + dt) * 64 + lane) * 4) = st.o[dt];
+        __syncthreads();
+        float im[NG];
+#pragma unroll
+        for (int u = 0; u < NG; u++) {
+            im[u] = sh.m[u * ROWS + rw * 16 + lr];
+            m = fmaxf(m, im[u]);
+        }
+        lsum = 0.f;
+#pragma unroll
+        for (int i = 0; i < OWN; i++) own[i] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < NG; u++) {
+            const float f = exp2f(im[u] - m);
+            lsum += sh.l[u * ROWS + rw * 16 + lr] * f;
+#pragma unroll
+            for (int i = 0; i < OWN; i++) own[i] += *reinterpret_cast<const float4_t*>(park + (((u * NR + rw) * DT + tg * OWN + i) * 64 + lane) * 4) * f;
         }
     }
-    constexpr int TB = NT < 2 ? NT : 2;
-    float* park = reinterpret_cast<float*>(smem);
+    const int dt0 = tg * OWN;   // the first tile of dims that this wavefront has
+
+    // The nodes' keys and values into the request's tail slots, which nobody reads in this launch: the last thing a workgroup does.  A thread takes
+    // 16 bytes of the four tokens that V keeps together in a page.
+    auto store_nodes = [&]() __attribute__((always_inline)) {
+        const int quad0 = L >> 2, quads = ((L + n + 3) >> 2) - quad0;
+        for (int e = tid; e < quads * CH; e += 64 * WAVES) {
+            const int pos0 = (quad0 + e / CH) * 4, d = e % CH * E;
+            const size_t at = ((layer_page + pages[pos0 >> 4]) * a.Hkv + g) * head;
+            T *kp = static_cast<T*>(a.k_pool) + at, *vp = static_cast<T*>(a.v_pool) + at;
+            union {
+                u32x4 u;
+                T x[E];
+            } kk[4], vv[4];
 #pragma unroll
-    for (int tb = 0; tb < NT; tb += TB) {
-        if (tb) __syncthreads();
-#pragma unroll
-        for (int u = 0; u < TB; u++)
-#pragma unroll
-            for (int dt = 0; dt < DT; dt++)
-                *reinterpret_cast<float4_t*>(park + (((u * WAVES + wave) * DT + dt) * 64 + lane) * 4) = st.o[tb + u][dt];
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < TB; u++) {
-            const int t = tb + u;
-            float f[WAVES];
-            m[t] = NEG_BIG;
-#pragma unroll
-            for (int v = 0; v < WAVES; v++) m[t] = fmaxf(m[t], sh_m[v][t * 16 + lr]);
-            lsum[t] = 0.f;
-#pragma unroll
-            for (int v = 0; v < WAVES; v++) {
-                f[v] = exp2f(sh_m[v][t * 16 + lr] - m[t]);
-                lsum[t] += sh_l[v][t * 16 + lr] * f[v];
+            for (int i = 0; i < 4; i++) {
+                const int j = min(max(pos0 + i - L, 0), n - 1);
+                kk[i].u = *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.k) + (size_t)(row0 + j) * a.k_stride + g * D + d);
+                vv[i].u = *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.v) + (size_t)(row0 + j) * a.v_stride + g * D + d);
             }
+            const bool whole = pos0 >= L && pos0 + 4 <= L + n;
 #pragma unroll
-            for (int i = 0; i < OWN; i++) {
-                own[t][i] = float4_t{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < 4; i++) {
+                const int slot = (pos0 & 15) + i;
+                if (pos0 + i < L || pos0 + i >= L + n) continue;
+                if constexpr (F32) {
+                    *reinterpret_cast<u32x4*>(kp + slot * D + d) = kk[i].u;
+                    *reinterpret_cast<u32x4*>(vp + slot * D + d) = vv[i].u;
+                } else {
+                    *reinterpret_cast<u32x4*>(kp + kpage_offset(slot, d)) = kk[i].u;
+                    if (!whole)
 #pragma unroll
-                for (int v = 0; v < WAVES; v++) {
-                    const float4_t x = *reinterpret_cast<const float4_t*>(park + (((u * WAVES + v) * DT + wave * OWN + i) * 64 + lane) * 4);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) own[t][i][e] += x[e] * f[v];
+                        for (int x = 0; x < 8; x++) vp[vpage_offset(slot, d + x)] = vv[i].x[x];
                 }
             }
+            if constexpr (!F32)
+                if (whole)
+#pragma unroll
+                    for (int x = 0; x < 8; x++)
+                        *reinterpret_cast<uint2*>(vp + vpage_offset(pos0 & 15, d + x)) =
+                            make_uint2((uint32_t)vv[0].x[x] | ((uint32_t)vv[1].x[x] << 16), (uint32_t)vv[2].x[x] | ((uint32_t)vv[3].x[x] << 16));
         }
-    }
+    };
+    const bool stores = last && r0 == 0;
 
-    uint32_t bad[2] = {sh_bad[0], sh_bad[1]};
+    uint32_t bad[2] = {sh.bad[0], sh.bad[1]};
     if (n_items > 1) {
         // Handing over without a device-wide fence: states are stored and read with device-scope accesses, and the counter is raised only
         // when this workgroup's stores have been acknowledged.
-        float* po = a.t.part_o + (size_t)w * (NT * DT * 256) + (wave * OWN) * 256 + lane;
-        float* pm = a.t.part_ml + (size_t)w * (2 * ROWS);
-#pragma unroll
-        for (int t = 0; t < NT; t++) {
-            if (wave == 0 && lg == 0) {
-                __hip_atomic_store(pm + t * 16 + lr, m[t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                __hip_atomic_store(pm + ROWS + t * 16 + lr, lsum[t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const size_t slot = slot0 + (size_t)(w - w0) * NR;   // of this item's first tile
+        float* po = a.t.part_o + (slot + rw) * (DT * 256) + dt0 * 256 + lane;
+        float* pm = a.t.part_ml + slot * 32 + rw * 16 + lr;
+        if (mine) {
+            if (tg == 0 && lg == 0) {
+                __hip_atomic_store(pm, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_store(pm + ROWS, lsum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
-            if (t >= n_tiles) continue;
 #pragma unroll
             for (int i = 0; i < OWN; i++)
 #pragma unroll
-                for (int e = 0; e < 4; e++)
-                    __hip_atomic_store(po + (t * DT + i) * 256 + e * 64, own[t][i][e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                for (int e = 0; e < 4; e++) __hip_atomic_store(po + i * 256 + e * 64, own[i][e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         uint32_t* arrive = reinterpret_cast<uint32_t*>(a.t.arrive + 4 * w0);   // counter, -, the two words of `bad`
-        if (last && tid < 2) __hip_atomic_store(arrive + 2 + tid, bad[tid & 1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (last && tid < 2) __hip_atomic_store(arrive + 2 + tid, tid ? bad[1] : bad[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         if (tid == 0) {
             const uint32_t old = __hip_atomic_fetch_add(arrive, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            sh_last = old == (uint32_t)n_items - 1;
-            if (sh_last) __hip_atomic_store(arrive, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next layer
+            sh.last = old == (uint32_t)n_items - 1;
+            if (sh.last) __hip_atomic_store(arrive, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next layer
         }
         __syncthreads();
-        if (!sh_last) return;
+        if (!sh.last) {
+            if (stores) store_nodes();
+            return;
+        }
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
         bad[0] = __hip_atomic_load(arrive + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         bad[1] = __hip_atomic_load(arrive + 3, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (mine) {
+            m = NEG_BIG;
+            lsum = 0.f;
 #pragma unroll
-        for (int t = 0; t < NT; t++) {
-            m[t] = NEG_BIG;
-            lsum[t] = 0.f;
+            for (int i = 0; i < OWN; i++) own[i] = float4_t{0.f, 0.f, 0.f, 0.f};
+            constexpr int AHEAD = 4;   // states asked for together
+            for (int c0 = 0; c0 < n_items; c0 += AHEAD) {   // in ascending order, whichever came last
+                float im[AHEAD], il[AHEAD], io[AHEAD][OWN][4];
 #pragma unroll
-            for (int i = 0; i < OWN; i++) own[t][i] = float4_t{0.f, 0.f, 0.f, 0.f};
-        }
-        for (int c = 0; c < n_items; c++) {   // in ascending order, whichever came last
-            const int wc = w0 + c * stride;
-            const float* qo = a.t.part_o + (size_t)wc * (NT * DT * 256) + (wave * OWN) * 256 + lane;
-            const float* qm = a.t.part_ml + (size_t)wc * (2 * ROWS);
-            float im[NT], il[NT], io[NT][OWN][4];
+                for (int c = 0; c < AHEAD; c++) {
+                    const size_t from = slot0 + (size_t)min(c0 + c, n_items - 1) * stride * NR;
+                    const float* qo = a.t.part_o + (from + rw) * (DT * 256) + dt0 * 256 + lane;
+                    const float* qm = a.t.part_ml + from * 32 + rw * 16 + lr;
+                    im[c] = __hip_atomic_load(qm, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    il[c] = __hip_atomic_load(qm + ROWS, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
-            for (int t = 0; t < NT; t++) {
-                im[t] = __hip_atomic_load(qm + t * 16 + lr, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                il[t] = __hip_atomic_load(qm + ROWS + t * 16 + lr, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    for (int i = 0; i < OWN; i++)
 #pragma unroll
-                for (int i = 0; i < OWN; i++)
+                        for (int e = 0; e < 4; e++) io[c][i][e] = __hip_atomic_load(qo + i * 256 + e * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
 #pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        io[t][i][e] = __hip_atomic_load(qo + (min(t, n_tiles - 1) * DT + i) * 256 + e * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
+                for (int c = 0; c < AHEAD; c++) {
+                    if (c0 + c >= n_items) continue;
+                    const float mnew = fmaxf(m, im[c]), fo = exp2f(m - mnew), fi = exp2f(im[c] - mnew);
+                    m = mnew;
+                    lsum = lsum * fo + il[c] * fi;
 #pragma unroll
-            for (int t = 0; t < NT; t++) {
-                const float mnew = fmaxf(m[t], im[t]), fo = exp2f(m[t] - mnew), fi = exp2f(im[t] - mnew);
-                m[t] = mnew;
-                lsum[t] = lsum[t] * fo + il[t] * fi;
+                    for (int i = 0; i < OWN; i++)
 #pragma unroll
-                for (int i = 0; i < OWN; i++)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) own[t][i][e] = own[t][i][e] * fo + io[t][i][e] * fi;
+                        for (int e = 0; e < 4; e++) own[i][e] = own[i][e] * fo + io[c][i][e] * fi;
+                }
             }
         }
     }
 
-    // the output: row lr of tile t, dims (wave * OWN + i) * 16 + lg * 4 ..
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-        const int r = r0 + t * 16 + lr;
-        if (r >= rows) continue;
-        const int j = r / G, h = g * G + r - j * G;
-        const float inv = 1.0f / lsum[t];
-        if (a.lse && wave == 0 && lg == 0) a.lse[(size_t)(row0 + j) * a.Hq + h] = (m[t] + log2f(lsum[t])) * 0.6931471805599453f;
-        const uint64_t poison = (bad[0] | bad[1]) ? a.t.seen[row0 + j] & (((uint64_t)bad[1] << 32) | bad[0]) : 0ull;
+    // the output: row lr of the tile, dims (dt0 + i) * 16 + lg * 4 ..
+    if (node < n) {
+        const int j = node, h = g * G + hh;
+        const float inv = 1.0f / lsum;
+        if (a.lse && tg == 0 && lg == 0) a.lse[(size_t)(row0 + j) * a.Hq + h] = (m + log2f(lsum)) * 0.6931471805599453f;
+        const uint64_t poison = (bad[0] | bad[1]) ? seen & (((uint64_t)bad[1] << 32) | bad[0]) : 0ull;
 #pragma unroll
         for (int i = 0; i < OWN; i++) {
-            const int d = (wave * OWN + i) * 16 + lg * 4;
+            const int d = (dt0 + i) * 16 + lg * 4;
             float y[4];
 #pragma unroll
-            for (int e = 0; e < 4; e++) y[e] = own[t][i][e] * inv;
+            for (int e = 0; e < 4; e++) y[e] = own[i][e] * inv;
             for (uint64_t left = poison; left; left &= left - 1) {   // values that are not finite, of nodes that this row sees
                 const T* vp = static_cast<const T*>(a.v) + (size_t)(row0 + __builtin_ctzll(left)) * a.v_stride + g * D + d;
 #pragma unroll
@@ -596,6 +744,19 @@ __global__ __launch_bounds__(64 * WAVES, 1) void tree_attention_kernel(tree_args
                 *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + ((size_t)(row0 + j) * a.Hq + h) * D + d) = z.u;
             }
         }
+    }
+    if (stores) store_nodes();
+}
+
+template <int D, bool F32, bool STEP>
+__global__ __launch_bounds__(64 * WAVES, 2) void tree_attention_kernel(tree_args a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    __shared__ tree_shared sh;
+    const int32_t* rec = a.t.items + SLED_TREE_ITEM * blockIdx.x;
+    switch (rec[13]) {
+        case 8: attend_item<8, D, F32, STEP>(a, rec, smem, sh); break;
+        case 4: attend_item<4, D, F32, STEP>(a, rec, smem, sh); break;
+        default: attend_item<2, D, F32, STEP>(a, rec, smem, sh);
     }
 }
 
@@ -644,7 +805,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void tree_mass_kernel(tree_args a,
         }
         __syncthreads();
         for (int p0 = page0 + wave * MP; p0 < page_end; p0 += MASS_WAVES * MP) {
-            KV<D, F32> kv[MP];   // (the values are never loaded)
+            Keys<D, F32> kv[MP];
 #pragma unroll
             for (int p = 0; p < MP; p++) {
                 const int phys = pages[min(p0 + p, page_end - 1)];
@@ -666,7 +827,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void tree_mass_kernel(tree_args a,
                     const float zz[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
                     for (int p = 0; p < MP; p++) {
-                        const float4_t s = page_scores<D, F32, PL, true>(kv[p], 0, qs + t * QT + lane);
+                        const float4_t s = page_scores<D, F32, PL>(kv[p], 0, qs + t * QT + lane);
                         float x = 0.f;
 #pragma unroll
                         for (int i = 0; i < 4; i++) {
@@ -763,27 +924,18 @@ __global__ __launch_bounds__(256) void tree_qkv_kernel(const float* __restrict__
     }
 }
 
-template <int NT, int D, bool F32, bool STEP>
+template <int D, bool F32, bool STEP>
 int launch_attention(const tree_args& a, hipStream_t st) {
-    constexpr size_t lds = attention_lds<NT, D, F32, (STEP && !F32 ? 2 : 1)>();
-    static_assert(lds <= 150 * 1024, "LDS of a workgroup");
+    constexpr size_t lds = std::max(attention_lds<2, D, F32>(), std::max(attention_lds<4, D, F32>(), attention_lds<8, D, F32>()));
+    static_assert(lds + sizeof(tree_shared) <= 160 * 1024, "LDS of a workgroup");
     static bool allowed = false;
     if (!allowed) {
-        SLED_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(tree_attention_kernel<NT, D, F32, STEP>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        SLED_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(tree_attention_kernel<D, F32, STEP>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
         allowed = true;
     }
-    hipLaunchKernelGGL((tree_attention_kernel<NT, D, F32, STEP>), dim3(a.t.n_items), dim3(64 * WAVES), lds, st, a);
+    hipLaunchKernelGGL((tree_attention_kernel<D, F32, STEP>), dim3(a.t.n_items), dim3(64 * WAVES), lds, st, a);
     SLED_LAUNCH_CHECK();
     return SLED_OK;
-}
-
-template <int D, bool F32, bool STEP>
-int launch_attention_tiles(const tree_args& a, hipStream_t st) {
-    switch (a.t.tiles) {
-        case 1: return launch_attention<1, D, F32, STEP>(a, st);
-        case 2: return launch_attention<2, D, F32, STEP>(a, st);
-        default: return launch_attention<4, D, F32, STEP>(a, st);
-    }
 }
 
 template <int D, bool F32, int PL>
@@ -829,8 +981,8 @@ int sled_launch_tree_attention(const sled_model* m, const sled_kvpool* p, const 
     a.out = out;
     a.x_plane = x_plane;
     a.lse = lse;
-    if (m->s.dtype == SLED_BF16) return step ? launch_attention_tiles<128, false, true>(a, st) : launch_attention_tiles<128, false, false>(a, st);
-    return m->s.head_dim == 64 ? launch_attention_tiles<64, true, false>(a, st) : launch_attention_tiles<128, true, false>(a, st);
+    if (m->s.dtype == SLED_BF16) return step ? launch_attention<128, false, true>(a, st) : launch_attention<128, false, false>(a, st);
+    return m->s.head_dim == 64 ? launch_attention<64, true, false>(a, st) : launch_attention<128, true, false>(a, st);
 }
 
 int sled_launch_tree_mass(const sled_model* m, const sled_kvpool* p, const sled_tree_plan& t, int layer, const void* q, size_t q_stride, size_t q_plane,
