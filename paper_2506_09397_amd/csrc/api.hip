@@ -1340,8 +1340,8 @@ struct tree_group {
 };
 // Wavefronts that share n row tiles; what is over works on other steps at the same time.
 int tree_waves(int n) { return n <= 2 ? 2 : n <= 4 ? 4 : 8; }
-// Time of a page in 1/16ths of one with all wavefronts on one step.
-int tree_page_cost(int waves) { return waves == 8 ? 16 : waves == 4 ? 10 : 7; }
+// Time of a page in 1/16ths of one with all wavefronts on one step, 850 clocks: measured 540 and 430 with four and two, more while memory is awaited.
+int tree_page_cost(int waves) { return waves == 8 ? 16 : waves == 4 ? 10 : 9; }
 int tree_chunk(const tree_group& x, int tgt, int P) {
     const int most = std::min(std::max(tgt * 16 / tree_page_cost(x.waves), P), SLED_TREE_RUN);
     return ceil_div(attn_chunk(std::max(x.pages, 1), most), P) * P;   // a step of the kernel is P pages
@@ -1351,12 +1351,12 @@ int tree_chunk(const tree_group& x, int tgt, int P) {
 // items of at most so long.  A launch of no more items than CUs takes as long as its longest; a longer one about its share of the whole on each CU and
 // half a longest item more.  An item's own start and end count as ITEM_FIXED pages and, where its context is split, ITEM_SPLIT more.
 int tree_item_length(const std::vector<tree_group>& groups, int Hkv, int P) {
-    constexpr int ITEM_FIXED = 12, ITEM_SPLIT = 6, LEAST = 8;
+    constexpr int ITEM_FIXED = 10, ITEM_SPLIT = 5, LEAST = 4;
     int longest = 1;
     for (const tree_group& x : groups) longest = std::max(longest, ceil_div(x.pages * tree_page_cost(x.waves), 16));
     int best = longest;
     double best_end = -1.0;
-    for (int tgt = longest; tgt == longest || tgt >= LEAST; tgt = std::min(tgt - 1, tgt * 7 / 8)) {
+    for (int tgt = longest; tgt == longest || tgt >= LEAST; tgt = std::min(tgt - 1, tgt * 4 / 5)) {
         int64_t items = 0;
         double total = 0.0, most = 0.0;
         for (const tree_group& x : groups) {

@@ -8,6 +8,7 @@ symbols fails loudly.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 from typing import Optional, Sequence
@@ -137,7 +138,8 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    """The current stream of the current device (torch.cuda.current_stream() without the object around it: 0.2 us instead of 2.9)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 # ---------------------------------------------------------------------------------------- model
@@ -304,13 +306,19 @@ def sled_profile_read(model: int):
 def _parents(n_nodes: Sequence[int], parents: Sequence[Sequence[int]]):
     """parents[i][j]: the node that node j of tree i continues (parents[i][0] is not looked at), packed."""
     assert len(parents) == len(n_nodes) and all(len(p) == n for p, n in zip(parents, n_nodes)), "a parent for every node of every tree"
-    return _ints([max(int(x), -1) if j else -1 for p in parents for j, x in enumerate(p)])
+    flat = array.array("i")
+    for p in parents:
+        if len(p):
+            flat.append(-1)
+            flat.extend(p[1:])
+    return (C.c_int * len(flat)).from_buffer(flat)
 
 
 def _rows(t: torch.Tensor):
     """(pointer, elements between rows) of a [T, heads, head_dim] tensor whose rows may lie apart."""
-    assert t.is_cuda and t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2], "rows of [heads, head_dim], each contiguous"
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    shape, stride = t.shape, t.stride()
+    assert t.is_cuda and len(shape) == 3 and stride[2] == 1 and stride[1] == shape[2], "rows of [heads, head_dim], each contiguous"
+    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
 
 def _bytes(t: torch.Tensor) -> int:
