@@ -4,251 +4,306 @@
 // node's uniform.  The child of c that drafted t is accepted and becomes c; if no child did, the walk ends and t is the answer.  Every token
 // that leaves is the target's own choice, so the text is the target's whatever the tree held.
 //
-// A walk needs the rows it passes and no others, and which those are is known one after the other.  Two forms:
-//   step by step   a launch per level of the tree.  Every request's workgroups first settle the level before (the pieces' results of that
-//                  row, the token, the child), each for itself, and then scan a piece of the child's row.  Nothing is handed over inside a launch.
-//   all rows       one launch that scans all rows of all trees, one that walks: where the rows are few.
-// Sums of exponentials are float64 in a fixed order, so a draw does not depend on how the row was cut.
+// A walk needs the rows it passes and no others, and which those are is known one after the other.  One workgroup of 16 wavefronts walks for a
+// request, in one launch: a row comes in at what one CU can draw, with up to 256 KB asked for at a time, and a walk costs what it is long.
+// Measured: 8 us a row of 128256 values (greedy), 22 us a row of 50257 (sampling, bound by one CU's float64 exponentials).  16 trees of
+// 333 nodes, up to 6 accepted: 61 us; 64 trees of 1946 nodes by sampling, up to 7 accepted: 180 us.  A launch per level of the trees, each row cut
+// into pieces for many CUs, took 86 and 288 us: it has to launch for the deepest tree, whose last nodes are hardly ever reached.
+// Sums of exponentials are float64 in a fixed order over the row, so a draw depends on nothing but its row.
 #include "sled_internal.h"
 
 #include <algorithm>
 
 namespace {
 
-constexpr int THREADS = 256, MAX_PIECES = 64;
-
-struct __align__(16) Piece {   // of a row
-    double sum;   // of exp((x - m) / tau) (sampling)
-    float m;      // largest logit
-    int arg;      // its lowest id
-};
+constexpr int THREADS = 1024, WAVES = THREADS / 64, ROUND = 16, AHEAD = 4;   // pieces of four values that a thread asks for at a time
 
 struct walk_args {
     const float* logits;
     const int32_t* tokens;
     const float* u;          // one per row (sampling)
     double inv_tau;
-    int V, pieces, seg, B;   // a row's pieces and their length
-    const uint8_t* parent;   // [T] (root: 255)
+    int V;
+    const uint8_t* parent;   // [T] (root: 255), where the shape does not come with the launch
     const int32_t* first;    // [B + 1] first row of a request
-    Piece* part;             // step by step: [2][B][pieces]; all rows: [T][pieces]
-    int32_t* cur;            // [2][B] node whose row was scanned last, -1: the walk has ended
     int32_t *accept_len, *path, *out_token;
 };
 
-__device__ inline void better(float& m, int& arg, float x, int i) {
-    if (x > m || (x == m && i < arg)) {
-        m = x;
-        arg = i;
-    }
-}
-
-// largest value and its lowest index over the workgroup, in every thread
-__device__ inline void block_max(float& m, int& arg, float* sh_m, int* sh_i) {
-    for (int off = 32; off > 0; off >>= 1) {
-        const float x = __shfl_xor(m, off);
-        const int i = __shfl_xor(arg, off);
-        better(m, arg, x, i);
-    }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) {
-        sh_m[threadIdx.x >> 6] = m;
-        sh_i[threadIdx.x >> 6] = arg;
-    }
-    __syncthreads();
-    m = sh_m[0];
-    arg = sh_i[0];
-    for (int w = 1; w < THREADS / 64; w++) better(m, arg, sh_m[w], sh_i[w]);
-}
-
-// piece s of a row -> *out
-template <bool SAMPLE>
-__device__ void scan_piece(const walk_args& a, const float* __restrict__ row, int s, Piece* out) {
-    __shared__ float sh_m[THREADS / 64];
-    __shared__ int sh_i[THREADS / 64];
-    __shared__ double sh_d[THREADS / 64];
-    const int lo = s * a.seg, hi = min(a.V, lo + a.seg), tid = threadIdx.x;
-    float m = -INFINITY;
-    int arg = 0x7fffffff;
-    int i = lo + tid;
-    for (; i + 7 * THREADS < hi; i += 8 * THREADS) {   // eight loads in flight
-        float x[8];
-#pragma unroll
-        for (int k = 0; k < 8; k++) x[k] = row[i + k * THREADS];
-#pragma unroll
-        for (int k = 0; k < 8; k++) better(m, arg, x[k], i + k * THREADS);
-    }
-    for (; i < hi; i += THREADS) better(m, arg, row[i], i);
-    block_max(m, arg, sh_m, sh_i);
-    double sum = 0.0;
-    if (SAMPLE) {
-        for (int k = lo + tid; k < hi; k += THREADS) sum += exp(((double)row[k] - (double)m) * a.inv_tau);
-        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
-        if ((tid & 63) == 0) sh_d[tid >> 6] = sum;
-        __syncthreads();
-        sum = 0.0;
-        for (int w = 0; w < THREADS / 64; w++) sum += sh_d[w];
-    }
-    if (tid == 0) *out = Piece{m > -INFINITY ? sum : 0.0, m, arg};
-}
-
-// the token that the target names behind a row, from the row's pieces; the whole workgroup takes part and gets it
-template <bool SAMPLE>
-__device__ int named_token(const walk_args& a, const float* __restrict__ row, const Piece* part, double u) {
-    __shared__ int sh_tok, sh_seg;
-    __shared__ double sh_rest, sh_wave[THREADS / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    __syncthreads();
-    Piece p{0.0, -INFINITY, 0x7fffffff};
-    if (lane < a.pieces) p = part[lane];
-    float m = p.m;
-    int arg = p.arg;
-    for (int off = 32; off > 0; off >>= 1) {
-        const float x = __shfl_xor(m, off);
-        const int i = __shfl_xor(arg, off);
-        better(m, arg, x, i);
-    }
-    if (!SAMPLE) return min(max(arg, 0), a.V - 1);
-    // the piece in which the cumulative sum passes u of the total
-    if (wave == 0) {
-        const double w = p.sum > 0.0 ? p.sum * exp(((double)p.m - (double)m) * a.inv_tau) : 0.0;
-        double c = w;
-        for (int off = 1; off < 64; off <<= 1) {
-            const double x = __shfl_up(c, off);
-            if (lane >= off) c += x;
-        }
-        const double target = u * __shfl(c, 63);
-        const uint64_t past = __ballot(c > target), some = __ballot(w > 0.0);
-        // none (rounding, or a row without a finite value): the last piece that holds anything
-        const int s = past ? __builtin_ctzll(past) : some ? 63 - __builtin_clzll(some) : 0;
-        const double before = __shfl(c, max(s - 1, 0));
-        if (lane == 0) {
-            sh_seg = s;
-            sh_rest = target - (s > 0 ? before : 0.0);
-        }
-    }
-    __syncthreads();
-    // within it, a run of neighbouring ids per thread
-    const int lo = sh_seg * a.seg, hi = min(a.V, lo + a.seg), per = (a.seg + THREADS - 1) / THREADS;
-    const double rest = sh_rest, md = (double)m;
-    const int k0 = min(hi, lo + tid * per), k1 = min(hi, k0 + per);
-    double mine = 0.0;
-    int last = -1;   // last id with mass
-    for (int k = k0; k < k1; k++) {
-        const double e = exp(((double)row[k] - md) * a.inv_tau);
-        mine += e;
-        if (e > 0.0) last = k;
-    }
-    double c = mine;
-    for (int off = 1; off < 64; off <<= 1) {
-        const double x = __shfl_up(c, off);
-        if (lane >= off) c += x;
-    }
-    if (lane == 63) sh_wave[wave] = c;
-    if (tid == 0) sh_tok = 0x7fffffff;
-    __syncthreads();
-    double base = 0.0;
-    for (int w = 0; w < wave; w++) base += sh_wave[w];
-    if (base + c > rest) {   // the sum passes in this thread's run or before it
-        double run = base + (c - mine);
-        int tok = last;
-        for (int k = k0; k < k1; k++) {
-            run += exp(((double)row[k] - md) * a.inv_tau);
-            if (run > rest) {
-                tok = k;
-                break;
-            }
-        }
-        if (tok >= 0) atomicMin(&sh_tok, tok);
-    }
-    __syncthreads();
-    int tok = sh_tok;
-    if (tok == 0x7fffffff) {   // it never passes: the last id with mass
-        __syncthreads();
-        if (tid == 0) sh_tok = -1;
-        __syncthreads();
-        if (last >= 0) atomicMax(&sh_tok, last);
-        __syncthreads();
-        tok = sh_tok;
-    }
-    return min(max(tok, 0), a.V - 1);
-}
-
-// the child of `cur` (a node of the request whose first row is row0) that drafted `tok`, the lowest if there are several, or -1
-__device__ inline int child_of(const walk_args& a, int row0, int n, int cur, int tok) {
-    const int lane = threadIdx.x & 63;
-    const bool hit = lane > 0 && lane < n && a.parent[row0 + min(lane, n - 1)] == cur && a.tokens[row0 + min(lane, n - 1)] == tok;
-    const uint64_t hits = __ballot(hit);
-    return hits ? __builtin_ctzll(hits) : -1;
-}
-
-// Level `level` of all walks: settle the level before, then scan a piece of the row of the node it led to.
-template <bool SAMPLE>
-__global__ __launch_bounds__(THREADS) void accept_tree_level(walk_args a, int level, int last_level) {
-    const int s = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-    const int row0 = a.first[b], n = a.first[b + 1] - row0;
-    int cur = 0;
-    if (level > 0) {
-        const int before = a.cur[((level - 1) & 1) * a.B + b];
-        cur = -1;
-        if (before >= 0) {
-            const float* row = a.logits + (size_t)(row0 + before) * a.V;
-            const int tok = named_token<SAMPLE>(a, row, a.part + ((size_t)((level - 1) & 1) * a.B + b) * a.pieces, SAMPLE ? (double)a.u[row0 + before] : 0.0);
-            cur = child_of(a, row0, n, before, tok);
-            if (s == 0 && tid == 0) {
-                if (cur >= 0) {
-                    a.path[(size_t)b * SLED_TREE_MAX + level - 1] = cur;
-                } else {
-                    a.accept_len[b] = level - 1;
-                    a.out_token[b] = tok;
-                }
-            }
-        }
-    }
-    if (s == 0 && tid == 0) a.cur[(level & 1) * a.B + b] = cur;
-    if (cur < 0 || last_level) return;
-    scan_piece<SAMPLE>(a, a.logits + (size_t)(row0 + cur) * a.V, s, a.part + ((size_t)(level & 1) * a.B + b) * a.pieces + s);
-}
-
-template <bool SAMPLE>
-__global__ __launch_bounds__(THREADS) void accept_tree_rows(walk_args a) {
-    const int s = blockIdx.x, t = blockIdx.y;
-    scan_piece<SAMPLE>(a, a.logits + (size_t)t * a.V, s, a.part + (size_t)t * a.pieces + s);
-}
-
-template <bool SAMPLE>
-__global__ __launch_bounds__(THREADS) void accept_tree_walk(walk_args a) {
-    const int b = blockIdx.x, row0 = a.first[b], n = a.first[b + 1] - row0;
-    int cur = 0;
-    for (int len = 0;; len++) {   // a child's number is larger than its parent's: at most n rounds
-        const size_t t = row0 + cur;
-        const int tok = named_token<SAMPLE>(a, a.logits + t * a.V, a.part + t * a.pieces, SAMPLE ? (double)a.u[t] : 0.0);
-        const int next = child_of(a, row0, n, cur, tok);
-        if (next < 0) {
-            if (threadIdx.x == 0) {
-                a.accept_len[b] = len;
-                a.out_token[b] = tok;
-            }
-            return;
-        }
-        if (threadIdx.x == 0) a.path[(size_t)b * SLED_TREE_MAX + len] = next;
-        cur = next;
-    }
-}
-
-// The trees' shape comes by value with the launch (so the call needs no copy from host memory and can be captured): the parents
-// in pieces, the sizes with the first.
+// The trees' shape comes by value with the launch (so the call needs no copy from host memory and can be captured).
 constexpr int PARENTS = 2048;
 struct __align__(16) Sizes {
-    uint8_t n[1024];   // nodes - 1
+    uint8_t n[1024];   // nodes - 1; 255 behind the last request
 };
 struct __align__(16) Parents {
     uint8_t p[PARENTS];
 };
-__global__ __launch_bounds__(256) void accept_tree_setup(Parents pp, int at, int count, uint8_t* __restrict__ parent) {
+
+struct Best {
+    float m;
+    int arg;
+};
+__device__ inline void better(Best& b, float x, int i) {
+    if (x > b.m || (x == b.m && i < b.arg)) {
+        b.m = x;
+        b.arg = i;
+    }
+}
+
+// four neighbouring values that start anywhere (a row is as aligned as its length)
+struct __attribute__((packed, aligned(4))) Four {
+    float x[4];
+};
+// The values at j .. j + 3 of a row of V >= 4, moved down where they would pass its end; returns where they begin
+__device__ inline int four_at(const float* __restrict__ row, int V, int j, Four& f) {
+    const int at = min(j, V - 4);
+    f = *reinterpret_cast<const Four*>(row + at);
+    return at;
+}
+
+// the same for a row of any length: what a short one lacks has no weight
+__device__ inline int four_of(const float* __restrict__ row, int V, int j, Four& f) {
+    if (V >= 4) return four_at(row, V, j, f);
+#pragma unroll
+    for (int e = 0; e < 4; e++) f.x[e] = e < V ? row[min(e, V - 1)] : -INFINITY;
+    return 0;
+}
+
+// e^y for y <= 0 (NaN stays one): y = k ln 2 + r, the Taylor series of e^r up to r^11 (|r| <= ln 2 / 2: the rest is below 7e-15 of it)
+__device__ inline double exp_below(double y) {
+    const double k = rint(y * 1.4426950408889634);
+    // ln 2 = 2977044471 / 2^32 + 1.908e-10: the first part times k is exact
+    const double r = fma(-k, 1.9082149292705877e-10, fma(-k, 2977044471.0 / 4294967296.0, y));
+    double e = 1.0 / 39916800;
+    e = fma(e, r, 1.0 / 3628800);
+    e = fma(e, r, 1.0 / 362880);
+    e = fma(e, r, 1.0 / 40320);
+    e = fma(e, r, 1.0 / 5040);
+    e = fma(e, r, 1.0 / 720);
+    e = fma(e, r, 1.0 / 120);
+    e = fma(e, r, 1.0 / 24);
+    e = fma(e, r, 1.0 / 6);
+    e = fma(e, r, 0.5);
+    e = fma(e, r, 1.0);
+    e = fma(e, r, 1.0);
+    return ldexp(e, (int)fmax(k, -1100.0));
+}
+// weight of a value; one that is not a number, or lies as far above as infinity, has none
+__device__ inline double weight(float x, double m, double inv_tau) {
+    const double e = exp_below(((double)x - m) * inv_tau);
+    return e > 0.0 ? e : 0.0;
+}
+
+struct walk_shared {
+    float m[WAVES];
+    int arg[WAVES];
+    double sum[WAVES];
+    int tok, last;
+};
+
+// largest value of a row and its lowest id, in every thread
+__device__ __forceinline__ Best row_best(const float* __restrict__ row, int V, walk_shared& sh) {
+    const int tid = threadIdx.x;
+    Best b{-INFINITY, 0x7fffffff};
+    if (V < 4) {
+        for (int k = 0; k < V; k++) better(b, row[k], k);
+        return b;
+    }
+    // A thread's pieces ascend, so only a larger value replaces one.  Which of a piece's four it was is found at the end.
+    int piece = 0;
+    for (int j0 = 0; j0 < V; j0 += ROUND * 4 * THREADS) {
+        Four f[ROUND];
+        int at[ROUND];
+#pragma unroll
+        for (int k = 0; k < ROUND; k++) at[k] = four_at(row, V, j0 + (k * THREADS + tid) * 4, f[k]);   // (some values twice, at the row's end)
+#pragma unroll
+        for (int k = 0; k < ROUND; k++) {
+            const float top = fmaxf(fmaxf(f[k].x[0], f[k].x[1]), fmaxf(f[k].x[2], f[k].x[3]));
+            if (top > b.m) {
+                b.m = top;
+                piece = at[k];
+            }
+        }
+    }
+    if (b.m > -INFINITY) {
+        Four f;
+        const int at = four_at(row, V, piece, f);
+        b.arg = f.x[0] == b.m ? at : f.x[1] == b.m ? at + 1 : f.x[2] == b.m ? at + 2 : at + 3;
+    } else {
+        b.arg = min(tid * 4, V - 4);   // nothing larger: the first of this thread's
+    }
+    for (int off = 32; off > 0; off >>= 1) {
+        const float x = __shfl_xor(b.m, off);
+        const int i = __shfl_xor(b.arg, off);
+        better(b, x, i);
+    }
+    __syncthreads();
+    if ((tid & 63) == 0) {
+        sh.m[tid >> 6] = b.m;
+        sh.arg[tid >> 6] = b.arg;
+    }
+    __syncthreads();
+    b = Best{sh.m[0], sh.arg[0]};
+#pragma unroll
+    for (int w = 1; w < WAVES; w++) better(b, sh.m[w], sh.arg[w]);
+    return b;
+}
+
+__device__ inline double sum_up_to_lane(double c, int lane) {
+    for (int off = 1; off < 64; off <<= 1) {
+        const double x = __shfl_up(c, off);
+        if (lane >= off) c += x;
+    }
+    return c;
+}
+
+// The id at which the cumulative sum of a row's weights passes u of their total.  A wavefront adds up a run of neighbouring ids; the run in which
+// the sum passes is then shared out among all threads.
+__device__ __forceinline__ int row_draw(const float* __restrict__ row, int V, const Best& b, double u, double inv_tau, walk_shared& sh) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const double m = (double)b.m;
+    const int run = (V + WAVES * 256 - 1) / (WAVES * 256) * 256, lo = min(V, wave * run), hi = min(V, lo + run);
+    double sum = 0.0;
+    if (V >= 4) {
+        Four next[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++) four_at(row, V, lo + k * 256 + lane * 4, next[k]);
+        for (int j0 = lo; j0 < hi; j0 += AHEAD * 256) {
+            Four f[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; k++) f[k] = next[k];
+#pragma unroll
+            for (int k = 0; k < AHEAD; k++) four_at(row, V, j0 + (AHEAD + k) * 256 + lane * 4, next[k]);
+#pragma unroll
+            for (int k = 0; k < AHEAD; k++) {
+                const int j = j0 + k * 256 + lane * 4, at = min(j, V - 4);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const double w = weight(f[k].x[e], m, inv_tau);
+                    sum += j < hi && at + e >= j ? w : 0.0;   // (a piece that was moved down: only what is its own)
+                }
+            }
+        }
+        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+    } else if (wave == 0) {
+        for (int k = 0; k < V; k++) sum += weight(row[k], m, inv_tau);
+    }
+    if (lane == 0) sh.sum[wave] = sum;
+    if (tid == 0) {
+        sh.tok = 0x7fffffff;
+        sh.last = -1;
+    }
+    __syncthreads();
+    double total = 0.0;
+#pragma unroll
+    for (int w = 0; w < WAVES; w++) total += sh.sum[w];
+    if (!(total > 0.0)) return b.arg;   // nothing weighs anything: a row without a finite value
+    const double target = u * total;
+    int s = -1, some = 0;
+    double before = 0.0, c = 0.0;
+#pragma unroll
+    for (int w = 0; w < WAVES; w++) {
+        const double x = sh.sum[w];
+        if (x > 0.0) some = w;
+        if (s < 0 && c + x > target) {
+            s = w;
+            before = c;
+        }
+        c += x;
+    }
+    if (s < 0) {   // it never passes (rounding): the last id with weight
+        s = some;
+        before = target;
+    }
+    const int from = min(V, s * run), to = min(V, from + run), per = (run + 4 * THREADS - 1) / (4 * THREADS) * 4;
+    const int k0 = min(to, from + tid * per), k1 = min(to, k0 + per);
+    double mine = 0.0;
+    int last = -1;
+    for (int k = k0; k < k1; k += 4) {
+        Four f;
+        const int at = four_of(row, V, k, f);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const double w = weight(f.x[e], m, inv_tau);
+            if (at + e < k || at + e >= k1 || !(w > 0.0)) continue;
+            mine += w;
+            last = at + e;
+        }
+    }
+    const double upto = sum_up_to_lane(mine, lane);
+    __syncthreads();   // the runs' sums have been read
+    if (lane == 63) sh.sum[wave] = upto;
+    __syncthreads();
+    double base = before;
+    for (int w = 0; w < wave; w++) base += sh.sum[w];
+    // the first thread that has weight and in whose ids, or before them, the sum passes
+    const uint64_t past = __ballot(base + upto > target && last >= 0), any = __ballot(last >= 0);
+    if (past && lane == __builtin_ctzll(past)) {
+        double at = base + (upto - mine);
+        int tok = last;
+        for (int k = k0; k < k1 && !(at > target); k += 4) {
+            Four f;
+            const int j = four_of(row, V, k, f);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                if (j + e < k || j + e >= k1 || at > target) continue;
+                at += weight(f.x[e], m, inv_tau);
+                if (at > target) tok = j + e;
+            }
+        }
+        atomicMin(&sh.tok, tok);
+    }
+    if (any && lane == 63 - __builtin_clzll(any)) atomicMax(&sh.last, last);
+    __syncthreads();
+    const int tok = sh.tok == 0x7fffffff ? sh.last : sh.tok;
+    __syncthreads();
+    return tok;
+}
+
+// SHAPE: the trees' shape is in sz and pp
+template <bool SAMPLE, bool SHAPE>
+__global__ __launch_bounds__(THREADS) void accept_tree_walk(walk_args a, Sizes sz, Parents pp) {
+    __shared__ walk_shared sh;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    int row0, n;
+    if (SHAPE) {
+        // nodes of the requests before: 16 sizes a lane
+        int sum = 0;
+#pragma unroll
+        for (int k = 0; k < 16; k++) sum += lane * 16 + k < b ? sz.n[lane * 16 + k] + 1 : 0;
+        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+        row0 = __builtin_amdgcn_readfirstlane(sum);
+        n = sz.n[b] + 1;
+    } else {
+        row0 = a.first[b];
+        n = a.first[b + 1] - row0;
+    }
+    // every wavefront has the whole tree: node `lane`
+    const int at = row0 + min(lane, n - 1), parent = SHAPE ? pp.p[at] : a.parent[at], token = a.tokens[at];
+    int cur = 0, way = -1;
+    for (int len = 0;; len++) {   // a child's number is larger than its parent's: at most n rounds
+        const float* row = a.logits + (size_t)(row0 + cur) * a.V;
+        const Best best = row_best(row, a.V, sh);
+        int tok = SAMPLE ? row_draw(row, a.V, best, (double)a.u[row0 + cur], a.inv_tau, sh) : best.arg;
+        tok = min(max(tok, 0), a.V - 1);
+        const uint64_t hits = __ballot(lane > 0 && lane < n && parent == cur && token == tok);   // (the lowest of several)
+        if (!hits) {
+            if (tid == 0) {
+                a.accept_len[b] = len;
+                a.out_token[b] = tok;
+            }
+            break;
+        }
+        cur = __builtin_ctzll(hits);
+        if (tid == len) way = cur;
+    }
+    if (tid < SLED_TREE_MAX) a.path[(size_t)b * SLED_TREE_MAX + tid] = way;
+}
+
+// Trees of more than PARENTS nodes in all: their shape goes to the workspace first.
+__global__ __launch_bounds__(256) void accept_tree_parents(Parents pp, int at, int count, uint8_t* __restrict__ parent) {
     for (int i = threadIdx.x; i < count; i += 256) parent[at + i] = pp.p[i];
 }
-__global__ __launch_bounds__(256) void accept_tree_first(Sizes sz, int B, int32_t* __restrict__ first, int32_t* __restrict__ path) {
+__global__ __launch_bounds__(256) void accept_tree_first(Sizes sz, int B, int32_t* __restrict__ first) {
     __shared__ int sh[256];
     const int tid = threadIdx.x;
     int n[4], sum = 0;
@@ -272,79 +327,42 @@ __global__ __launch_bounds__(256) void accept_tree_first(Sizes sz, int B, int32_
         at += n[k];
     }
     if (tid == 255 && B == 1024) first[1024] = at;
-    for (int i = tid; i < B * SLED_TREE_MAX; i += 256) path[i] = -1;
 }
 
-int pick_pieces(int rows, int V) {
-    // about 1024 workgroups a launch, none of less than 2048 values
-    const int n = std::max(1, std::min(MAX_PIECES, 1024 / std::max(1, rows)));
-    return std::max(1, std::min(n, V / 2048));
-}
-bool all_rows(int B, int T, int depth, int V) {
-    (void)B;
-    return (int64_t)T * V * 4 <= (int64_t)depth * (8 << 20);
-}
 size_t up(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
 
-size_t sled_accept_tree_ws_bytes(int B, int T, int vocab) {
-    const size_t parts = std::max((size_t)2 * B * pick_pieces(B, vocab), (size_t)T * pick_pieces(T, vocab)) * sizeof(Piece);
-    return up(parts) + up((size_t)2 * B * 4) + up((size_t)(B + 1) * 4) + up(T);
-}
+size_t sled_accept_tree_ws_bytes(int B, int T) { return up((size_t)(B + 1) * 4) + up(T); }
 
-int sled_launch_accept_tree(int mode, int B, int T, const int* n_nodes, const int* parent, int depth, int vocab, float temperature, const float* logits,
+int sled_launch_accept_tree(int mode, int B, int T, const int* n_nodes, const int* parent, int vocab, float temperature, const float* logits,
                             const int32_t* tokens, const float* u, int32_t* accept_len, int32_t* path, int32_t* out_token, void* ws, hipStream_t st) {
-    walk_args a{};
-    a.logits = logits;
-    a.tokens = tokens;
-    a.u = u;
-    a.inv_tau = 1.0 / (double)temperature;
-    a.V = vocab;
-    a.B = B;
-    const bool rows = all_rows(B, T, depth + 1, vocab);
-    a.pieces = pick_pieces(rows ? T : B, vocab);
-    a.seg = (vocab + a.pieces - 1) / a.pieces;
     char* w = static_cast<char*>(ws);
-    a.part = reinterpret_cast<Piece*>(w);
-    w += up(std::max((size_t)2 * B * pick_pieces(B, vocab), (size_t)T * pick_pieces(T, vocab)) * sizeof(Piece));
-    a.cur = reinterpret_cast<int32_t*>(w);
-    w += up((size_t)2 * B * 4);
     int32_t* first = reinterpret_cast<int32_t*>(w);
-    w += up((size_t)(B + 1) * 4);
-    uint8_t* par = reinterpret_cast<uint8_t*>(w);
-    a.first = first;
-    a.parent = par;
-    a.accept_len = accept_len;
-    a.path = path;
-    a.out_token = out_token;
+    uint8_t* par = reinterpret_cast<uint8_t*>(w + up((size_t)(B + 1) * 4));
+    const walk_args a{logits, tokens, u, 1.0 / (double)temperature, vocab, par, first, accept_len, path, out_token};
     Sizes sz;
-    for (int i = 0; i < 1024; i++) sz.n[i] = i < B ? (uint8_t)(n_nodes[i] - 1) : 0;
-    hipLaunchKernelGGL(accept_tree_first, dim3(1), dim3(256), 0, st, sz, B, first, path);
+    for (int i = 0; i < 1024; i++) sz.n[i] = i < B ? (uint8_t)(n_nodes[i] - 1) : 255;
+    Parents pp;
+    auto fill = [&](int at, int count) {
+        for (int i = 0; i < count; i++) pp.p[i] = parent[at + i] >= 0 ? (uint8_t)parent[at + i] : 255;
+    };
+    const bool sample = mode == SLED_SAMPLE, shape = T <= PARENTS;
+    if (!shape) {
+        hipLaunchKernelGGL(accept_tree_first, dim3(1), dim3(256), 0, st, sz, B, first);
+        SLED_LAUNCH_CHECK();
+        for (int at = 0; at < T; at += PARENTS) {
+            const int count = std::min(PARENTS, T - at);
+            fill(at, count);
+            hipLaunchKernelGGL(accept_tree_parents, dim3(1), dim3(256), 0, st, pp, at, count, par);
+            SLED_LAUNCH_CHECK();
+        }
+    } else {
+        fill(0, T);
+    }
+    auto kernel = sample ? (shape ? accept_tree_walk<true, true> : accept_tree_walk<true, false>)
+                         : (shape ? accept_tree_walk<false, true> : accept_tree_walk<false, false>);
+    hipLaunchKernelGGL(kernel, dim3(B), dim3(THREADS), 0, st, a, sz, pp);
     SLED_LAUNCH_CHECK();
-    for (int at = 0; at < T; at += PARENTS) {
-        Parents pp;
-        const int count = std::min(PARENTS, T - at);
-        for (int i = 0; i < PARENTS; i++) pp.p[i] = i < count && parent[at + i] >= 0 ? (uint8_t)parent[at + i] : 255;
-        hipLaunchKernelGGL(accept_tree_setup, dim3(1), dim3(256), 0, st, pp, at, count, par);
-        SLED_LAUNCH_CHECK();
-    }
-    const bool sample = mode == SLED_SAMPLE;
-    if (rows) {
-        if (sample) hipLaunchKernelGGL(accept_tree_rows<true>, dim3(a.pieces, T), dim3(THREADS), 0, st, a);
-        else hipLaunchKernelGGL(accept_tree_rows<false>, dim3(a.pieces, T), dim3(THREADS), 0, st, a);
-        SLED_LAUNCH_CHECK();
-        if (sample) hipLaunchKernelGGL(accept_tree_walk<true>, dim3(B), dim3(THREADS), 0, st, a);
-        else hipLaunchKernelGGL(accept_tree_walk<false>, dim3(B), dim3(THREADS), 0, st, a);
-        SLED_LAUNCH_CHECK();
-        return SLED_OK;
-    }
-    for (int level = 0; level <= depth + 1; level++) {
-        const bool last = level == depth + 1;
-        const dim3 grid(last ? 1 : a.pieces, B);
-        if (sample) hipLaunchKernelGGL(accept_tree_level<true>, grid, dim3(THREADS), 0, st, a, level, (int)last);
-        else hipLaunchKernelGGL(accept_tree_level<false>, grid, dim3(THREADS), 0, st, a, level, (int)last);
-        SLED_LAUNCH_CHECK();
-    }
     return SLED_OK;
 }
