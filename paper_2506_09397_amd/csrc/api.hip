@@ -1270,7 +1270,7 @@ int refuse_capture(hipStream_t st, const char* who) {
     return SLED_OK;
 }
 
-constexpr int MASS_ITEM_PAGES = 32;   // of a workgroup of the mass kernel: four for each of its eight wavefronts
+constexpr int MASS_ITEM_PAGES = 16;   // of a workgroup of the mass kernel: two for each of its eight wavefronts
 
 // a plan in the caller's workspace
 struct tree_layout {

@@ -200,19 +200,28 @@ struct tree_args {
     float* lse;                // or nullptr
 };
 
-// Copies rows r0 .. r0 + n_rows - 1 of a block's stacked rows into LDS, as the operand pieces of their tiles; rows from `rows` on are zero
-template <int D, bool F32, int PL>
-__device__ __forceinline__ void stage_queries(u32x4* qs, const tree_args& a, int row0, int g, int G, int r0, int n_rows, int rows, int tid, int nt) {
+// Rows r0 .. r0 + n_rows - 1 of a block's stacked rows on their way into LDS, as the operand pieces of their tiles: a thread's pieces e0, e0 + nt, ...
+template <int D, bool F32, int PL, int N>
+__device__ __forceinline__ void ask_queries(u32x4 (&x)[N], const tree_args& a, int row0, int g, int G, int r0, int rows, int e0, int nt) {
     constexpr int CH = D * Geo<D, F32>::ELEM / 16;   // 16-byte pieces of a row
-    for (int e = tid; e < n_rows * PL * CH; e += nt) {
-        const int c = e % CH, pl = e / CH % PL, rr = e / (CH * PL);
-        u32x4 x = {0u, 0u, 0u, 0u};
-        if (r0 + rr < rows) {
-            const int j = (r0 + rr) / G, hh = (r0 + rr) - j * G;
-            const size_t at = (pl * a.q_plane + (size_t)(row0 + j) * a.q_stride + (size_t)(g * G + hh) * D) * Geo<D, F32>::ELEM + c * 16;
-            x = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) + at);
-        }
-        qs[((rr >> 4) * PL + pl) * CH * 16 + q_piece<F32>(rr & 15, c)] = x;
+    asm volatile("" : "+v"(e0));   // (addresses are made when they are needed: kept, they would cost registers)
+#pragma unroll
+    for (int u = 0; u < N; u++) {
+        const int e = e0 + u * nt, c = e % CH, pl = e / CH % PL, r = min(r0 + e / (CH * PL), rows - 1);   // (any row that there is)
+        const int j = r / G, hh = r - j * G;
+        const size_t at = (pl * a.q_plane + (size_t)(row0 + j) * a.q_stride + (size_t)(g * G + hh) * D) * Geo<D, F32>::ELEM + c * 16;
+        x[u] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) + at);
+    }
+}
+// ... and there; rows from `rows` on are zero
+template <int D, bool F32, int PL, int N>
+__device__ __forceinline__ void put_queries(u32x4* qs, const u32x4 (&x)[N], int r0, int n_rows, int rows, int e0, int nt) {
+    constexpr int CH = D * Geo<D, F32>::ELEM / 16;
+    asm volatile("" : "+v"(e0));
+#pragma unroll
+    for (int u = 0; u < N; u++) {
+        const int e = e0 + u * nt, c = e % CH, pl = e / CH % PL, rr = e / (CH * PL);
+        if (rr < n_rows) qs[((rr >> 4) * PL + pl) * CH * 16 + q_piece<F32>(rr & 15, c)] = r0 + rr < rows ? x[u] : u32x4{0u, 0u, 0u, 0u};
     }
 }
 
@@ -767,7 +776,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_attention_kernel(tree_args
 // lane group in a fixed order: no atomics, and the same result every time.
 constexpr int MASS_WAVES = 8;
 template <bool F32>
-__host__ __device__ constexpr int mass_pages() { return F32 ? 2 : 4; }   // pages of a wavefront at a time
+__host__ __device__ constexpr int mass_pages() { return 2; }   // pages of a wavefront at a time
 __host__ __device__ constexpr int mass_rows(int PL) { return PL == 1 ? 256 : 128; }   // rows in LDS at a time
 
 struct mass_args {
@@ -775,8 +784,9 @@ struct mass_args {
     int cap, n_layers;
 };
 
+// (two workgroups a CU where the registers allow it)
 template <int D, bool F32, int PL>
-__global__ __launch_bounds__(64 * MASS_WAVES) void tree_mass_kernel(tree_args a, mass_args ma) {
+__global__ __launch_bounds__(64 * MASS_WAVES, PL == 1 && !F32 ? 4 : 2) void tree_mass_kernel(tree_args a, mass_args ma) {
     constexpr int MP = mass_pages<F32>(), QT = Geo<D, F32>::QC * 64 * PL, MR = mass_rows(PL);
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -793,42 +803,69 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void tree_mass_kernel(tree_args a,
     uint64_t* seen = reinterpret_cast<uint64_t*>(lse2 + room);
     const size_t head = (size_t)16 * D, layer_page = (size_t)a.layer * a.n_pages;
     using T = std::conditional_t<F32, float, bf16_t>;
-    for (int r0 = 0; r0 < rows; r0 += MR) {
-        const int n_rows = min(MR, (rows - r0 + 15) & ~15);
-        if (r0) __syncthreads();
-        stage_queries<D, F32, PL>(qs, a, row0, g, G, r0, n_rows, rows, tid, 64 * MASS_WAVES);
-        for (int r = tid; r < n_rows; r += 64 * MASS_WAVES) {
-            const int j = (r0 + r) / G, h = g * G + (r0 + r) - j * G;
-            // a row that does not exist has an infinite denominator: its weights are zero
-            lse2[r] = r0 + r < rows ? a.lse[(size_t)(row0 + j) * a.Hq + h] * 1.4426950408889634f : INFINITY;
-            seen[r] = r0 + r < rows ? a.t.seen[row0 + j] : 0ull;
-        }
-        __syncthreads();
-        for (int p0 = page0 + wave * MP; p0 < page_end; p0 += MASS_WAVES * MP) {
-            Keys<D, F32> kv[MP];
+    constexpr int CHUNK = D * Geo<D, F32>::ELEM / 16 * PL, NT = 64 * MASS_WAVES, ASK = 4;
+    static_assert(MR <= NT, "a thread for every row");
+    for (int pb = page0; pb < page_end; pb += MASS_WAVES * MP) {
+        const int p0 = pb + wave * MP;   // this wavefront's pages
+        const bool stage_first = rows > MR || pb == page0;   // (rows that all fit stay where they are)
+        if (pb > page0) __syncthreads();
+        // Rows are asked for before they are needed: the first before the keys, so that they can be put in place while the keys are still on
+        // their way, the next before the products with those in LDS.
+        u32x4 x[ASK];
+        float lse = 0.f;
+        uint64_t sees = 0;
+        auto ask = [&](int r0) __attribute__((always_inline)) {
+            ask_queries<D, F32, PL>(x, a, row0, g, G, r0, rows, tid, NT);
+            const int r = min(r0 + tid, rows - 1), j = r / G, h = g * G + r - j * G;
+            lse = a.lse[(size_t)(row0 + j) * a.Hq + h];
+            sees = a.t.seen[row0 + j];
+        };
+        if (stage_first) ask(0);
+        Keys<D, F32> kv[MP];
+        float* row = ma.mass + (((size_t)req * ma.n_layers + a.layer) * a.Hkv + g) * ma.cap;
+        float had[MP], acc[MP];
 #pragma unroll
-            for (int p = 0; p < MP; p++) {
-                const int phys = pages[min(p0 + p, page_end - 1)];
-                const T* kp = static_cast<const T*>(a.k_pool) + ((layer_page + phys) * a.Hkv + g) * head;
-                if constexpr (!F32) {
+        for (int p = 0; p < MP; p++) {
+            const int phys = pages[min(p0 + p, page_end - 1)];
+            const T* kp = static_cast<const T*>(a.k_pool) + ((layer_page + phys) * a.Hkv + g) * head;
+            if constexpr (!F32) {
 #pragma unroll
-                    for (int c = 0; c < 4; c++) kv[p].k[0][c] = reinterpret_cast<const u32x4*>(kp)[c * 64 + lane];
-                } else {
+                for (int c = 0; c < 4; c++) kv[p].k[0][c] = reinterpret_cast<const u32x4*>(kp)[c * 64 + lane];
+            } else {
 #pragma unroll
-                    for (int c = 0; c < D / 16; c++) kv[p].k[c] = *reinterpret_cast<const f32x4*>(kp + lr * D + lg * 4 + 16 * c);
-                }
+                for (int c = 0; c < D / 16; c++) kv[p].k[c] = *reinterpret_cast<const f32x4*>(kp + lr * D + lg * 4 + 16 * c);
             }
-            float acc[MP];
-#pragma unroll
-            for (int p = 0; p < MP; p++) acc[p] = 0.f;
-            auto walk = [&](auto masked) {
+            // a node's slot holds no mass of its own yet, but perhaps that of a node that was not accepted
+            const int pos = (p0 + p) * 16 + lr;
+            had[p] = pos < L ? row[pos] : 0.f;
+            acc[p] = 0.f;
+        }
+        for (int r0 = 0; r0 < rows; r0 += MR) {
+            const int n_rows = min(MR, (rows - r0 + 15) & ~15);
+            if (r0 || stage_first) {
+                if (r0) __syncthreads();
+                put_queries<D, F32, PL>(qs, x, r0, n_rows, rows, tid, NT);
+                for (int e0 = tid + ASK * NT; e0 < n_rows * CHUNK; e0 += ASK * NT) {
+                    ask_queries<D, F32, PL>(x, a, row0, g, G, r0, rows, e0, NT);
+                    put_queries<D, F32, PL>(qs, x, r0, n_rows, rows, e0, NT);
+                }
+                if (tid < n_rows) {
+                    // a row that does not exist has an infinite denominator: its weights are zero
+                    lse2[tid] = r0 + tid < rows ? lse * 1.4426950408889634f : INFINITY;
+                    seen[tid] = r0 + tid < rows ? sees : 0ull;
+                }
+                __syncthreads();
+                if (r0 + MR < rows) ask(r0 + MR);
+            }
+            if (p0 >= page_end) continue;
+            auto walk = [&](auto masked) __attribute__((always_inline)) {
                 for (int t = 0; t < n_rows / 16; t++) {
                     const float4 z = *reinterpret_cast<const float4*>(lse2 + t * 16 + lg * 4);   // of the rows this lane has
                     const float zz[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
                     for (int p = 0; p < MP; p++) {
                         const float4_t s = page_scores<D, F32, PL>(kv[p], 0, qs + t * QT + lane);
-                        float x = 0.f;
+                        float sum = 0.f;
 #pragma unroll
                         for (int i = 0; i < 4; i++) {
                             float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -zz[i]));
@@ -837,25 +874,21 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void tree_mass_kernel(tree_args a,
                                 const bool on = c < 0 || (c < n && ((seen[t * 16 + lg * 4 + i] >> (c & 63)) & 1ull));
                                 e = on ? e : 0.f;
                             }
-                            x += e;
+                            sum = i ? sum + e : e;
                         }
-                        acc[p] += x;
+                        acc[p] += sum;
                     }
                 }
             };
             if ((p0 + MP) * 16 > L) walk(std::true_type{});
             else walk(std::false_type{});
-            float* row = ma.mass + (((size_t)req * ma.n_layers + a.layer) * a.Hkv + g) * ma.cap;
+        }
+        if (p0 >= page_end) continue;
 #pragma unroll
-            for (int p = 0; p < MP; p++) {
-                const float x = sum_over_groups(acc[p]);
-                const int pos = (p0 + p) * 16 + lr;
-                if (lg == 0 && p0 + p < page_end && pos < L + n) {
-                    // a node's slot holds no mass of its own yet, but perhaps that of a node that was not accepted
-                    if (pos < L || r0) row[pos] += x;
-                    else row[pos] = x;
-                }
-            }
+        for (int p = 0; p < MP; p++) {
+            const float sum = sum_over_groups(acc[p]);
+            const int pos = (p0 + p) * 16 + lr;
+            if (lg == 0 && p0 + p < page_end && pos < L + n) row[pos] = had[p] + sum;
         }
     }
 }
