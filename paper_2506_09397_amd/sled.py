@@ -314,9 +314,9 @@ def _parents(n_nodes: Sequence[int], parents: Sequence[Sequence[int]]):
     return (C.c_int * len(flat)).from_buffer(flat)
 
 
-def _rows(t: torch.Tensor):
+def _rows(t: torch.Tensor, shape: Sequence[int]):
     """(pointer, elements between rows) of a [T, heads, head_dim] tensor whose rows may lie apart."""
-    shape, stride = t.shape, t.stride()
+    stride = t.stride()
     assert t.is_cuda and len(shape) == 3 and stride[2] == 1 and stride[1] == shape[2], "rows of [heads, head_dim], each contiguous"
     return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
@@ -344,14 +344,15 @@ def sled_tree_begin(pool: int, req_ids: Sequence[int], n_nodes: Sequence[int], p
 
 def sled_tree_attention(pool: int, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor],
                         workspace: torch.Tensor) -> None:
-    assert q.dtype == k.dtype == v.dtype == out.dtype and (lse is None or lse.dtype == torch.float32)
-    assert q.shape[0] == k.shape[0] == v.shape[0] and k.shape == v.shape and out.shape == q.shape and (lse is None or lse.shape == q.shape[:2])
-    _check(lib().sled_tree_attention(pool, int(layer), *_rows(q), *_rows(k), *_rows(v), _ptr(out), _ptr(lse), _ptr(workspace), _stream()))
+    rows, kv_rows, dtype = q.shape, k.shape, q.dtype
+    assert k.dtype is dtype and v.dtype is dtype and out.dtype is dtype and (lse is None or lse.dtype is torch.float32)
+    assert rows[0] == kv_rows[0] and v.shape == kv_rows and out.shape == rows and (lse is None or lse.shape == rows[:2])
+    _check(lib().sled_tree_attention(pool, int(layer), *_rows(q, rows), *_rows(k, kv_rows), *_rows(v, kv_rows), _ptr(out), _ptr(lse), _ptr(workspace), _stream()))
 
 
 def sled_tree_mass(pool: int, layer: int, q: torch.Tensor, lse: torch.Tensor, mass: torch.Tensor, workspace: torch.Tensor) -> None:
     assert lse.dtype == torch.float32 and lse.shape == q.shape[:2]
-    _check(lib().sled_tree_mass(pool, int(layer), *_rows(q), _ptr(lse), *_mass(mass), _ptr(workspace), _stream()))
+    _check(lib().sled_tree_mass(pool, int(layer), *_rows(q, q.shape), _ptr(lse), *_mass(mass), _ptr(workspace), _stream()))
 
 
 def sled_tree_commit(pool: int, req_ids: Sequence[int], accept_len: torch.Tensor, path: torch.Tensor, mass: Optional[torch.Tensor] = None) -> None:
