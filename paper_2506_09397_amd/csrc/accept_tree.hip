@@ -114,9 +114,11 @@ __device__ __forceinline__ Best row_best(const float* __restrict__ row, int V, w
         Four f[ROUND];
         int at[ROUND];
 #pragma unroll
-        for (int k = 0; k < ROUND; k++) at[k] = four_at(row, V, j0 + (k * THREADS + tid) * 4, f[k]);   // (some values twice, at the row's end)
+        for (int k = 0; k < ROUND; k++)
+            if (j0 + k * THREADS * 4 < V) at[k] = four_at(row, V, j0 + (k * THREADS + tid) * 4, f[k]);   // (some values twice, at the row's end)
 #pragma unroll
         for (int k = 0; k < ROUND; k++) {
+            if (j0 + k * THREADS * 4 >= V) break;
             const float top = fmaxf(fmaxf(f[k].x[0], f[k].x[1]), fmaxf(f[k].x[2], f[k].x[3]));
             if (top > b.m) {
                 b.m = top;

@@ -303,6 +303,11 @@ def sled_profile_read(model: int):
 
 
 # ---------------------------------------------------------------------------------------- trees of drafts, eviction
+def _packed(xs: Sequence[int]):
+    a = array.array("i", xs)
+    return (C.c_int * len(a)).from_buffer(a)
+
+
 def _parents(n_nodes: Sequence[int], parents: Sequence[Sequence[int]]):
     """parents[i][j]: the node that node j of tree i continues (parents[i][0] is not looked at), packed."""
     assert len(parents) == len(n_nodes) and all(len(p) == n for p, n in zip(parents, n_nodes)), "a parent for every node of every tree"
@@ -339,7 +344,7 @@ def sled_tree_workspace_bytes(model: int, B_max: int, T_max: int, ctx_tokens_max
 
 def sled_tree_begin(pool: int, req_ids: Sequence[int], n_nodes: Sequence[int], parents: Sequence[Sequence[int]], workspace: torch.Tensor) -> None:
     assert len(req_ids) == len(n_nodes)
-    _check(lib().sled_tree_begin(pool, len(req_ids), _ints(req_ids), _ints(n_nodes), _parents(n_nodes, parents), _ptr(workspace), _bytes(workspace), _stream()))
+    _check(lib().sled_tree_begin(pool, len(req_ids), _packed(req_ids), _packed(n_nodes), _parents(n_nodes, parents), _ptr(workspace), _bytes(workspace), _stream()))
 
 
 def sled_tree_attention(pool: int, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor],
@@ -357,7 +362,7 @@ def sled_tree_mass(pool: int, layer: int, q: torch.Tensor, lse: torch.Tensor, ma
 
 def sled_tree_commit(pool: int, req_ids: Sequence[int], accept_len: torch.Tensor, path: torch.Tensor, mass: Optional[torch.Tensor] = None) -> None:
     assert accept_len.dtype == torch.int32 and path.dtype == torch.int32 and tuple(path.shape) == (len(req_ids), TREE_MAX) and accept_len.numel() == len(req_ids)
-    _check(lib().sled_tree_commit(pool, len(req_ids), _ints(req_ids), _ptr(accept_len), _ptr(path), *_mass(mass), _stream()))
+    _check(lib().sled_tree_commit(pool, len(req_ids), _packed(req_ids), _ptr(accept_len), _ptr(path), *_mass(mass), _stream()))
 
 
 def sled_verify_tree_workspace_bytes(model: int, B_max: int, T_max: int, ctx_tokens_max: int) -> int:
@@ -368,7 +373,7 @@ def sled_verify_tree(model: int, pool: int, req_ids: Sequence[int], n_nodes: Seq
                      logits: torch.Tensor, workspace: torch.Tensor, mass: Optional[torch.Tensor] = None) -> None:
     assert tokens.dtype == torch.int32 and logits.dtype == torch.float32 and len(req_ids) == len(n_nodes)
     assert tokens.numel() == sum(n_nodes) and logits.shape[0] == sum(n_nodes)
-    _check(lib().sled_verify_tree(model, pool, len(req_ids), _ints(req_ids), _ints(n_nodes), _parents(n_nodes, parents), _ptr(tokens), _ptr(logits), *_mass(mass),
+    _check(lib().sled_verify_tree(model, pool, len(req_ids), _packed(req_ids), _packed(n_nodes), _parents(n_nodes, parents), _ptr(tokens), _ptr(logits), *_mass(mass),
                                   _ptr(workspace), _bytes(workspace), _stream()))
 
 
@@ -379,12 +384,12 @@ def sled_accept_tree_workspace_bytes(B: int, T: int, vocab: int) -> int:
 def sled_accept_tree(mode: int, n_nodes: Sequence[int], parents: Sequence[Sequence[int]], vocab: int, temperature: float, logits: torch.Tensor,
                      tokens: torch.Tensor, u: Optional[torch.Tensor], accept_len: torch.Tensor, path: torch.Tensor, out_token: torch.Tensor,
                      workspace: torch.Tensor) -> None:
-    T = sum(n_nodes)
-    assert logits.dtype == torch.float32 and tuple(logits.shape) == (T, vocab) and tokens.dtype == torch.int32 and tokens.numel() == T
-    assert u is None or (u.dtype == torch.float32 and u.numel() == T)
-    assert accept_len.dtype == torch.int32 and out_token.dtype == torch.int32 and path.dtype == torch.int32 and tuple(path.shape) == (len(n_nodes), TREE_MAX)
-    assert accept_len.numel() == out_token.numel() == len(n_nodes)
-    _check(lib().sled_accept_tree(mode, len(n_nodes), _ints(n_nodes), _parents(n_nodes, parents), vocab, float(temperature), _ptr(logits), _ptr(tokens), _ptr(u),
+    B, T, ints, floats = len(n_nodes), sum(n_nodes), torch.int32, torch.float32
+    assert logits.dtype is floats and logits.shape == (T, vocab) and tokens.dtype is ints and tokens.numel() == T
+    assert u is None or (u.dtype is floats and u.numel() == T)
+    assert accept_len.dtype is ints and out_token.dtype is ints and path.dtype is ints and path.shape == (B, TREE_MAX)
+    assert accept_len.numel() == out_token.numel() == B
+    _check(lib().sled_accept_tree(mode, B, _packed(n_nodes), _parents(n_nodes, parents), vocab, temperature, _ptr(logits), _ptr(tokens), _ptr(u),
                                   _ptr(accept_len), _ptr(path), _ptr(out_token), _ptr(workspace), _bytes(workspace), _stream()))
 
 
@@ -395,13 +400,13 @@ def sled_kv_evict_workspace_bytes(model: int, B_max: int, keep_max: int) -> int:
 def sled_kv_evict(pool: int, req_ids: Sequence[int], keep: Sequence[int], n_first: int, n_recent: int, mass: torch.Tensor, workspace: torch.Tensor,
                   dst_ids: Optional[Sequence[int]] = None) -> None:
     assert len(keep) == len(req_ids) and (dst_ids is None or len(dst_ids) == len(req_ids))
-    _check(lib().sled_kv_evict(pool, len(req_ids), _ints(req_ids), None if dst_ids is None else _ints(dst_ids), _ints(keep), int(n_first), int(n_recent),
+    _check(lib().sled_kv_evict(pool, len(req_ids), _packed(req_ids), None if dst_ids is None else _packed(dst_ids), _packed(keep), int(n_first), int(n_recent),
                                *_mass(mass), _ptr(workspace), _bytes(workspace), _stream()))
 
 
 def sled_kvpool_positions(pool: int, req_ids: Sequence[int]):
     out = (C.c_int * len(req_ids))()
-    _check(lib().sled_kvpool_positions(pool, len(req_ids), _ints(req_ids), out, _stream()))
+    _check(lib().sled_kvpool_positions(pool, len(req_ids), _packed(req_ids), out, _stream()))
     return list(out)
 
 
