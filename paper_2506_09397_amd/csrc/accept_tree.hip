@@ -12,7 +12,10 @@
 // Sums of exponentials are float64 in a fixed order over the row, so a draw depends on nothing but its row.
 #include "sled_internal.h"
 
+#include <string.h>
+
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -31,12 +34,13 @@ struct walk_args {
 
 // The trees' shape comes by value with the launch (so the call needs no copy from host memory and can be captured).
 constexpr int PARENTS = 2048;
-struct __align__(16) Sizes {
-    uint8_t n[1024];   // nodes - 1; 255 behind the last request
+template <int B, int T>
+struct __align__(16) Shape {
+    uint8_t n[B];   // nodes - 1
+    uint8_t p[T];   // parents (root: 255)
 };
-struct __align__(16) Parents {
-    uint8_t p[PARENTS];
-};
+typedef Shape<64, 256> Small;
+typedef Shape<1024, PARENTS> Large;
 
 struct Best {
     float m;
@@ -261,26 +265,31 @@ __device__ __forceinline__ int row_draw(const float* __restrict__ row, int V, co
     return tok;
 }
 
-// SHAPE: the trees' shape is in sz and pp
-template <bool SAMPLE, bool SHAPE>
-__global__ __launch_bounds__(THREADS) void accept_tree_walk(walk_args a, Sizes sz, Parents pp) {
+struct Stored {};   // the shape is in a.first and a.parent
+
+template <bool SAMPLE, class S>
+__global__ __launch_bounds__(THREADS) void accept_tree_walk(walk_args a, S shape) {
     __shared__ walk_shared sh;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     int row0, n;
-    if (SHAPE) {
-        // nodes of the requests before: 16 sizes a lane
+    if constexpr (!std::is_same_v<S, Stored>) {
+        // nodes of the requests before
+        constexpr int EACH = sizeof(shape.n) / 64;
         int sum = 0;
 #pragma unroll
-        for (int k = 0; k < 16; k++) sum += lane * 16 + k < b ? sz.n[lane * 16 + k] + 1 : 0;
+        for (int k = 0; k < EACH; k++) sum += lane * EACH + k < b ? shape.n[lane * EACH + k] + 1 : 0;
         for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
         row0 = __builtin_amdgcn_readfirstlane(sum);
-        n = sz.n[b] + 1;
+        n = shape.n[b] + 1;
     } else {
         row0 = a.first[b];
         n = a.first[b + 1] - row0;
     }
     // every wavefront has the whole tree: node `lane`
-    const int at = row0 + min(lane, n - 1), parent = SHAPE ? pp.p[at] : a.parent[at], token = a.tokens[at];
+    const int at = row0 + min(lane, n - 1), token = a.tokens[at];
+    int parent;
+    if constexpr (!std::is_same_v<S, Stored>) parent = shape.p[at];
+    else parent = a.parent[at];
     int cur = 0, way = -1;
     for (int len = 0;; len++) {   // a child's number is larger than its parent's: at most n rounds
         const float* row = a.logits + (size_t)(row0 + cur) * a.V;
@@ -302,16 +311,16 @@ __global__ __launch_bounds__(THREADS) void accept_tree_walk(walk_args a, Sizes s
 }
 
 // Trees of more than PARENTS nodes in all: their shape goes to the workspace first.
-__global__ __launch_bounds__(256) void accept_tree_parents(Parents pp, int at, int count, uint8_t* __restrict__ parent) {
-    for (int i = threadIdx.x; i < count; i += 256) parent[at + i] = pp.p[i];
+__global__ __launch_bounds__(256) void accept_tree_parents(Large x, int at, int count, uint8_t* __restrict__ parent) {
+    for (int i = threadIdx.x; i < count; i += 256) parent[at + i] = x.p[i];
 }
-__global__ __launch_bounds__(256) void accept_tree_first(Sizes sz, int B, int32_t* __restrict__ first) {
+__global__ __launch_bounds__(256) void accept_tree_first(Large x, int B, int32_t* __restrict__ first) {
     __shared__ int sh[256];
     const int tid = threadIdx.x;
     int n[4], sum = 0;
 #pragma unroll
     for (int k = 0; k < 4; k++) {
-        n[k] = 4 * tid + k < B ? sz.n[4 * tid + k] + 1 : 0;
+        n[k] = 4 * tid + k < B ? x.n[4 * tid + k] + 1 : 0;
         sum += n[k];
     }
     sh[tid] = sum;
@@ -343,28 +352,38 @@ int sled_launch_accept_tree(int mode, int B, int T, const int* n_nodes, const in
     int32_t* first = reinterpret_cast<int32_t*>(w);
     uint8_t* par = reinterpret_cast<uint8_t*>(w + up((size_t)(B + 1) * 4));
     const walk_args a{logits, tokens, u, 1.0 / (double)temperature, vocab, par, first, accept_len, path, out_token};
-    Sizes sz;
-    for (int i = 0; i < 1024; i++) sz.n[i] = i < B ? (uint8_t)(n_nodes[i] - 1) : 255;
-    Parents pp;
-    auto fill = [&](int at, int count) {
-        for (int i = 0; i < count; i++) pp.p[i] = parent[at + i] >= 0 ? (uint8_t)parent[at + i] : 255;
+    const bool sample = mode == SLED_SAMPLE;
+    auto fill = [&](auto& x, int at, int count) {
+        memset(&x, 0, sizeof(x));
+        for (int i = 0; i < B; i++) x.n[i] = (uint8_t)(n_nodes[i] - 1);
+        for (int i = 0; i < count; i++) x.p[i] = parent[at + i] >= 0 ? (uint8_t)parent[at + i] : 255;
     };
-    const bool sample = mode == SLED_SAMPLE, shape = T <= PARENTS;
-    if (!shape) {
-        hipLaunchKernelGGL(accept_tree_first, dim3(1), dim3(256), 0, st, sz, B, first);
-        SLED_LAUNCH_CHECK();
+    auto walk = [&](auto x) {
+        using S = decltype(x);
+        if (sample) hipLaunchKernelGGL((accept_tree_walk<true, S>), dim3(B), dim3(THREADS), 0, st, a, x);
+        else hipLaunchKernelGGL((accept_tree_walk<false, S>), dim3(B), dim3(THREADS), 0, st, a, x);
+    };
+    // (a launch with 320 bytes of arguments costs the host 4 us less than one with 3 KB: one tree of 9 nodes 9 us instead of 14 in all)
+    if (B <= 64 && T <= 256) {
+        Small x;
+        fill(x, 0, T);
+        walk(x);
+    } else if (T <= PARENTS) {
+        Large x;
+        fill(x, 0, T);
+        walk(x);
+    } else {
+        Large x;
         for (int at = 0; at < T; at += PARENTS) {
             const int count = std::min(PARENTS, T - at);
-            fill(at, count);
-            hipLaunchKernelGGL(accept_tree_parents, dim3(1), dim3(256), 0, st, pp, at, count, par);
+            fill(x, at, count);
+            if (at == 0) hipLaunchKernelGGL(accept_tree_first, dim3(1), dim3(256), 0, st, x, B, first);
+            SLED_LAUNCH_CHECK();
+            hipLaunchKernelGGL(accept_tree_parents, dim3(1), dim3(256), 0, st, x, at, count, par);
             SLED_LAUNCH_CHECK();
         }
-    } else {
-        fill(0, T);
+        walk(Stored{});
     }
-    auto kernel = sample ? (shape ? accept_tree_walk<true, true> : accept_tree_walk<true, false>)
-                         : (shape ? accept_tree_walk<false, true> : accept_tree_walk<false, false>);
-    hipLaunchKernelGGL(kernel, dim3(B), dim3(THREADS), 0, st, a, sz, pp);
     SLED_LAUNCH_CHECK();
     return SLED_OK;
 }
