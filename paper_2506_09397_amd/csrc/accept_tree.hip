@@ -4,12 +4,14 @@
 // node's uniform.  The child of c that drafted t is accepted and becomes c; if no child did, the walk ends and t is the answer.  Every token
 // that leaves is the target's own choice, so the text is the target's whatever the tree held.
 //
-// A walk needs the rows it passes and no others, and which those are is known one after the other.  One workgroup of 16 wavefronts walks for a
-// request, in one launch: a row comes in at what one CU can draw, with up to 256 KB asked for at a time, and a walk costs what it is long.
-// Measured: 8 us a row of 128256 values (greedy), 22 us a row of 50257 (sampling, bound by one CU's float64 exponentials).  16 trees of
-// 333 nodes, up to 6 accepted: 61 us; 64 trees of 1946 nodes by sampling, up to 7 accepted: 180 us.  A launch per level of the trees, each row cut
-// into pieces for many CUs, took 86 and 288 us: it has to launch for the deepest tree, whose last nodes are hardly ever reached.
-// Sums of exponentials are float64 in a fixed order over the row, so a draw depends on nothing but its row.
+// A walk needs the rows it passes and no others, and which those are is known one after the other.
+//   few rows    one launch scans all rows of all trees in pieces (largest logit, its lowest id, sum of the weights); a workgroup per request then walks
+//               in what that left, 1 us a node (greedy) or 8 (sampling: the piece in which the sum passes is gone through once more).
+//   many rows   one launch: a workgroup of 16 wavefronts walks for a request and goes through each row by itself, with up to 256 KB asked for at a
+//               time: 8 us a row of 128256 values out of L2, 14 out of memory; by sampling 22 us a row of 50257, one CU's float64 exponentials.
+// 16 trees of 333 nodes, 128256 values, up to 6 accepted: 37 us; 64 trees of 1946 nodes by sampling, 50257 values, up to 7 accepted: 190 us.  A launch per
+// level of the trees took 86 and 288 us: it has to launch for the deepest tree, whose last nodes are hardly ever reached.
+// Sums of exponentials are float64 in a fixed order over the row: what rounding leaves between the forms is 1e-14 of the sum.
 #include "sled_internal.h"
 
 #include <string.h>
@@ -21,6 +23,7 @@ namespace {
 
 constexpr int THREADS = 1024, WAVES = THREADS / 64, ROUND = 16, AHEAD = 4;   // pieces of four values that a thread asks for at a time
 
+struct Piece;
 struct walk_args {
     const float* logits;
     const int32_t* tokens;
@@ -30,6 +33,14 @@ struct walk_args {
     const uint8_t* parent;   // [T] (root: 255), where the shape does not come with the launch
     const int32_t* first;    // [B + 1] first row of a request
     int32_t *accept_len, *path, *out_token;
+    Piece* part;      // [T][pieces], where the rows have been scanned already
+    int pieces, seg;         // of a row, and their length
+};
+
+struct __align__(16) Piece {   // of a row
+    double sum;   // weights against its own largest logit (sampling)
+    float m;      // largest logit
+    int arg;      // its lowest id
 };
 
 // The trees' shape comes by value with the launch (so the call needs no copy from host memory and can be captured).
@@ -162,6 +173,58 @@ __device__ inline double sum_up_to_lane(double c, int lane) {
     return c;
 }
 
+// The id of the run of n ids from `from` on at which the cumulative sum, `before` up to there, passes the target; or the run's last id with weight
+__device__ __forceinline__ int draw_within(const float* __restrict__ row, int V, int from, int n, double before, double target, double m, double inv_tau, walk_shared& sh) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (n + 4 * THREADS - 1) / (4 * THREADS) * 4;
+    from = min(V, from);
+    const int to = min(V, from + n), k0 = min(to, from + tid * per), k1 = min(to, k0 + per);
+    double mine = 0.0;
+    int last = -1;
+    for (int k = k0; k < k1; k += 4) {
+        Four f;
+        const int at = four_of(row, V, k, f);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const double w = weight(f.x[e], m, inv_tau);
+            if (at + e < k || at + e >= k1 || !(w > 0.0)) continue;
+            mine += w;
+            last = at + e;
+        }
+    }
+    const double upto = sum_up_to_lane(mine, lane);
+    __syncthreads();   // (what the caller has in sh.sum has been read)
+    if (tid == 0) {
+        sh.tok = 0x7fffffff;
+        sh.last = -1;
+    }
+    if (lane == 63) sh.sum[wave] = upto;
+    __syncthreads();
+    double base = before;
+    for (int w = 0; w < wave; w++) base += sh.sum[w];
+    // the first thread that has weight and in whose ids, or before them, the sum passes
+    const uint64_t past = __ballot(base + upto > target && last >= 0), any = __ballot(last >= 0);
+    if (past && lane == __builtin_ctzll(past)) {
+        double at = base + (upto - mine);
+        int tok = last;
+        for (int k = k0; k < k1 && !(at > target); k += 4) {
+            Four f;
+            const int j = four_of(row, V, k, f);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                if (j + e < k || j + e >= k1 || at > target) continue;
+                at += weight(f.x[e], m, inv_tau);
+                if (at > target) tok = j + e;
+            }
+        }
+        atomicMin(&sh.tok, tok);
+    }
+    if (any && lane == 63 - __builtin_clzll(any)) atomicMax(&sh.last, last);
+    __syncthreads();
+    const int tok = sh.tok == 0x7fffffff ? sh.last : sh.tok;
+    __syncthreads();
+    return tok;
+}
+
 // The id at which the cumulative sum of a row's weights passes u of their total.  A wavefront adds up a run of neighbouring ids; the run in which
 // the sum passes is then shared out among all threads.
 __device__ __forceinline__ int row_draw(const float* __restrict__ row, int V, const Best& b, double u, double inv_tau, walk_shared& sh) {
@@ -194,10 +257,6 @@ __device__ __forceinline__ int row_draw(const float* __restrict__ row, int V, co
         for (int k = 0; k < V; k++) sum += weight(row[k], m, inv_tau);
     }
     if (lane == 0) sh.sum[wave] = sum;
-    if (tid == 0) {
-        sh.tok = 0x7fffffff;
-        sh.last = -1;
-    }
     __syncthreads();
     double total = 0.0;
 #pragma unroll
@@ -220,54 +279,95 @@ __device__ __forceinline__ int row_draw(const float* __restrict__ row, int V, co
         s = some;
         before = target;
     }
-    const int from = min(V, s * run), to = min(V, from + run), per = (run + 4 * THREADS - 1) / (4 * THREADS) * 4;
-    const int k0 = min(to, from + tid * per), k1 = min(to, k0 + per);
-    double mine = 0.0;
-    int last = -1;
-    for (int k = k0; k < k1; k += 4) {
-        Four f;
-        const int at = four_of(row, V, k, f);
+    return draw_within(row, V, s * run, run, before, target, m, inv_tau, sh);
+}
+
+// Where there are few rows: all of them are scanned in pieces by a launch of its own, and the walk finds its tokens in what that left.
+constexpr int SCAN_THREADS = 256;
+template <bool SAMPLE>
+__global__ __launch_bounds__(SCAN_THREADS) void accept_tree_scan(walk_args a) {
+    __shared__ float sh_m[SCAN_THREADS / 64];
+    __shared__ int sh_i[SCAN_THREADS / 64];
+    __shared__ double sh_d[SCAN_THREADS / 64];
+    const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V;
+    const size_t t = blockIdx.y;
+    const float* row = a.logits + t * V;
+    const int lo = s * a.seg, hi = min(V, lo + a.seg);   // (V is no less than 4, and lo less than V)
+    Best b{-INFINITY, 0x7fffffff};
+    for (int j0 = lo; j0 < hi; j0 += AHEAD * 4 * SCAN_THREADS) {
+        Four f[AHEAD];
+        int at[AHEAD];
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const double w = weight(f.x[e], m, inv_tau);
-            if (at + e < k || at + e >= k1 || !(w > 0.0)) continue;
-            mine += w;
-            last = at + e;
-        }
+        for (int k = 0; k < AHEAD; k++) at[k] = four_at(row, V, j0 + (k * SCAN_THREADS + tid) * 4, f[k]);
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (at[k] + e >= lo && at[k] + e < hi) better(b, f[k].x[e], at[k] + e);
     }
-    const double upto = sum_up_to_lane(mine, lane);
-    __syncthreads();   // the runs' sums have been read
-    if (lane == 63) sh.sum[wave] = upto;
+    for (int off = 32; off > 0; off >>= 1) {
+        const float x = __shfl_xor(b.m, off);
+        const int i = __shfl_xor(b.arg, off);
+        better(b, x, i);
+    }
+    if (lane == 0) {
+        sh_m[wave] = b.m;
+        sh_i[wave] = b.arg;
+    }
     __syncthreads();
-    double base = before;
-    for (int w = 0; w < wave; w++) base += sh.sum[w];
-    // the first thread that has weight and in whose ids, or before them, the sum passes
-    const uint64_t past = __ballot(base + upto > target && last >= 0), any = __ballot(last >= 0);
-    if (past && lane == __builtin_ctzll(past)) {
-        double at = base + (upto - mine);
-        int tok = last;
-        for (int k = k0; k < k1 && !(at > target); k += 4) {
+    b = Best{sh_m[0], sh_i[0]};
+#pragma unroll
+    for (int w = 1; w < SCAN_THREADS / 64; w++) better(b, sh_m[w], sh_i[w]);
+    double sum = 0.0;
+    if (SAMPLE) {
+        for (int j0 = lo + tid * 4; j0 < hi; j0 += 4 * SCAN_THREADS) {
             Four f;
-            const int j = four_of(row, V, k, f);
+            const int at = four_at(row, V, j0, f);
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                if (j + e < k || j + e >= k1 || at > target) continue;
-                at += weight(f.x[e], m, inv_tau);
-                if (at > target) tok = j + e;
+                const double w = weight(f.x[e], (double)b.m, a.inv_tau);
+                sum += at + e >= j0 && at + e < hi ? w : 0.0;
             }
         }
-        atomicMin(&sh.tok, tok);
+        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+        if (lane == 0) sh_d[wave] = sum;
+        __syncthreads();
+        sum = 0.0;
+#pragma unroll
+        for (int w = 0; w < SCAN_THREADS / 64; w++) sum += sh_d[w];
     }
-    if (any && lane == 63 - __builtin_clzll(any)) atomicMax(&sh.last, last);
-    __syncthreads();
-    const int tok = sh.tok == 0x7fffffff ? sh.last : sh.tok;
-    __syncthreads();
-    return tok;
+    if (tid == 0) a.part[t * a.pieces + s] = Piece{sum, b.m, b.arg};
+}
+
+// the token of a row whose pieces are at hand: a lane for each, in every wavefront
+template <bool SAMPLE>
+__device__ __forceinline__ int row_token(const walk_args& a, size_t t, walk_shared& sh) {
+    const int lane = threadIdx.x & 63;
+    Piece p{0.0, -INFINITY, 0x7fffffff};
+    if (lane < a.pieces) p = a.part[t * a.pieces + lane];
+    Best b{p.m, p.arg};
+    for (int off = 32; off > 0; off >>= 1) {
+        const float x = __shfl_xor(b.m, off);
+        const int i = __shfl_xor(b.arg, off);
+        better(b, x, i);
+    }
+    if constexpr (!SAMPLE) return b.arg;
+    const double w = p.sum > 0.0 ? p.sum * exp_below(((double)p.m - (double)b.m) * a.inv_tau) : 0.0, c = sum_up_to_lane(w, lane), total = __shfl(c, 63);
+    if (!(total > 0.0)) return b.arg;
+    double target = (double)a.u[t] * total;
+    const uint64_t past = __ballot(c > target), some = __ballot(w > 0.0);
+    const int s = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);   // (it never passes: the last with weight)
+    double before = __shfl(c, max(s - 1, 0));
+    if (s == 0) before = 0.0;
+    // against the row's largest logit a piece weighs what it does against its own, times a factor: the sums of its ids are compared in the latter
+    const double own = (double)__shfl(p.m, s), scale = exp_below((own - (double)b.m) * a.inv_tau);
+    return draw_within(a.logits + t * a.V, a.V, s * a.seg, a.seg, past ? before / scale : 0.0, past ? target / scale : INFINITY, own, a.inv_tau, sh);
 }
 
 struct Stored {};   // the shape is in a.first and a.parent
 
-template <bool SAMPLE, class S>
+// SCANNED: the rows' pieces are at hand
+template <bool SAMPLE, class S, bool SCANNED>
 __global__ __launch_bounds__(THREADS) void accept_tree_walk(walk_args a, S shape) {
     __shared__ walk_shared sh;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
@@ -293,8 +393,13 @@ __global__ __launch_bounds__(THREADS) void accept_tree_walk(walk_args a, S shape
     int cur = 0, way = -1;
     for (int len = 0;; len++) {   // a child's number is larger than its parent's: at most n rounds
         const float* row = a.logits + (size_t)(row0 + cur) * a.V;
-        const Best best = row_best(row, a.V, sh);
-        int tok = SAMPLE ? row_draw(row, a.V, best, (double)a.u[row0 + cur], a.inv_tau, sh) : best.arg;
+        int tok;
+        if constexpr (SCANNED) {
+            tok = row_token<SAMPLE>(a, row0 + cur, sh);
+        } else {
+            const Best best = row_best(row, a.V, sh);
+            tok = SAMPLE ? row_draw(row, a.V, best, (double)a.u[row0 + cur], a.inv_tau, sh) : best.arg;
+        }
         tok = min(max(tok, 0), a.V - 1);
         const uint64_t hits = __ballot(lane > 0 && lane < n && parent == cur && token == tok);   // (the lowest of several)
         if (!hits) {
@@ -342,17 +447,37 @@ __global__ __launch_bounds__(256) void accept_tree_first(Large x, int B, int32_t
 
 size_t up(size_t x) { return (x + 255) / 256 * 256; }
 
+// Scanning all rows first costs what they hold at the rate of the whole card, walking alone what the longest walk passes at the rate of one CU.  Measured
+// with walks of up to 8 nodes, 50257 values, scanned first / alone: 1024 rows 104 / 112 us (sampling 166 / 277), 1536 rows 146 / 127 (216 / 272),
+// 1920 rows 168 / 124 (251 / 253).  One tree of 9 rows of 128256 values 19 / 51 (36 / 132), of 1024 values 21 / 33 us.
+constexpr int SCAN_ROWS = 1024, SCAN_ROWS_SAMPLE = 1536;
+static_assert(PARENTS >= SCAN_ROWS_SAMPLE, "the shape of few rows travels with the launch");
+bool scan_first(bool sample, int T, int V) { return V >= 4 && T <= (sample ? SCAN_ROWS_SAMPLE : SCAN_ROWS); }
+// pieces of at least 4096 values, and no more than a wavefront has lanes
+int seg_of(int V) { return std::max(4096, (V + 63) / 64 + 1023) / 1024 * 1024; }
+int pieces_of(int V) { return (V + seg_of(V) - 1) / seg_of(V); }
+
 }  // namespace
 
-size_t sled_accept_tree_ws_bytes(int B, int T) { return up((size_t)(B + 1) * 4) + up(T); }
+size_t sled_accept_tree_ws_bytes(int B, int T, int vocab) {
+    const size_t part = scan_first(true, T, vocab) ? (size_t)T * pieces_of(vocab) * sizeof(Piece) : 0;
+    return up(part) + up((size_t)(B + 1) * 4) + up(T);
+}
 
 int sled_launch_accept_tree(int mode, int B, int T, const int* n_nodes, const int* parent, int vocab, float temperature, const float* logits,
                             const int32_t* tokens, const float* u, int32_t* accept_len, int32_t* path, int32_t* out_token, void* ws, hipStream_t st) {
+    const bool sample = mode == SLED_SAMPLE, scan = scan_first(sample, T, vocab);
     char* w = static_cast<char*>(ws);
     int32_t* first = reinterpret_cast<int32_t*>(w);
-    uint8_t* par = reinterpret_cast<uint8_t*>(w + up((size_t)(B + 1) * 4));
-    const walk_args a{logits, tokens, u, 1.0 / (double)temperature, vocab, par, first, accept_len, path, out_token};
-    const bool sample = mode == SLED_SAMPLE;
+    w += up((size_t)(B + 1) * 4);
+    uint8_t* par = reinterpret_cast<uint8_t*>(w);
+    w += up(T);
+    const walk_args a{logits, tokens, u, 1.0 / (double)temperature, vocab, par, first, accept_len, path, out_token, reinterpret_cast<Piece*>(w), pieces_of(vocab), seg_of(vocab)};
+    if (scan) {
+        if (sample) hipLaunchKernelGGL(accept_tree_scan<true>, dim3(a.pieces, T), dim3(SCAN_THREADS), 0, st, a);
+        else hipLaunchKernelGGL(accept_tree_scan<false>, dim3(a.pieces, T), dim3(SCAN_THREADS), 0, st, a);
+        SLED_LAUNCH_CHECK();
+    }
     auto fill = [&](auto& x, int at, int count) {
         memset(&x, 0, sizeof(x));
         for (int i = 0; i < B; i++) x.n[i] = (uint8_t)(n_nodes[i] - 1);
@@ -360,8 +485,10 @@ int sled_launch_accept_tree(int mode, int B, int T, const int* n_nodes, const in
     };
     auto walk = [&](auto x) {
         using S = decltype(x);
-        if (sample) hipLaunchKernelGGL((accept_tree_walk<true, S>), dim3(B), dim3(THREADS), 0, st, a, x);
-        else hipLaunchKernelGGL((accept_tree_walk<false, S>), dim3(B), dim3(THREADS), 0, st, a, x);
+        auto kernel = sample ? accept_tree_walk<true, S, false> : accept_tree_walk<false, S, false>;
+        if constexpr (!std::is_same_v<S, Stored>)   // (there are few rows where they are scanned first)
+            if (scan) kernel = sample ? accept_tree_walk<true, S, true> : accept_tree_walk<false, S, true>;
+        hipLaunchKernelGGL(kernel, dim3(B), dim3(scan && !sample ? 64 : THREADS), 0, st, a, x);
     };
     // (a launch with 320 bytes of arguments costs the host 4 us less than one with 3 KB: one tree of 9 nodes 9 us instead of 14 in all)
     if (B <= 64 && T <= 256) {

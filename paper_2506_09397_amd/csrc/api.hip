@@ -1644,7 +1644,7 @@ SLED_CATCH("sled_verify_tree")
 
 extern "C" size_t sled_accept_tree_workspace_bytes(int B, int T, int vocab) {
     if (B < 1 || T < 1 || vocab < 2) return 0;
-    return sled_accept_tree_ws_bytes(B, T);
+    return sled_accept_tree_ws_bytes(B, T, vocab);
 }
 
 extern "C" int sled_accept_tree(int mode, int B, const int* n_nodes, const int* parent, int vocab, float temperature, const float* logits, const int32_t* tokens,
@@ -1659,7 +1659,7 @@ extern "C" int sled_accept_tree(int mode, int B, const int* n_nodes, const int* 
     int rc = check_trees(B, n_nodes, parent, &T, nullptr, nullptr, "sled_accept_tree");
     if (rc != SLED_OK) return rc;
     if (reinterpret_cast<uintptr_t>(workspace) % 256) SLED_FAIL(SLED_EINVAL, "sled_accept_tree: workspace must be 256-byte aligned");
-    const size_t need = sled_accept_tree_ws_bytes(B, T);
+    const size_t need = sled_accept_tree_ws_bytes(B, T, vocab);
     if (need > workspace_bytes) SLED_FAIL(SLED_EINVAL, "sled_accept_tree: workspace of %zu bytes, %zu needed", workspace_bytes, need);
     return sled_launch_accept_tree(mode, B, T, n_nodes, parent, vocab, temperature, logits, tokens, u, accept_len, path, out_token, workspace,
                                    static_cast<hipStream_t>(stream));

@@ -320,7 +320,7 @@ int sled_launch_tree_commit(const sled_model* m, const sled_kvpool* p, const int
                             const int32_t* path, float* mass, int cap, hipStream_t st);
 
 // accept_tree.hip
-size_t sled_accept_tree_ws_bytes(int B, int T);
+size_t sled_accept_tree_ws_bytes(int B, int T, int vocab);
 int sled_launch_accept_tree(int mode, int B, int T, const int* n_nodes, const int* parent, int vocab, float temperature, const float* logits,
                             const int32_t* tokens, const float* u, int32_t* accept_len, int32_t* path, int32_t* out_token, void* ws, hipStream_t st);
 

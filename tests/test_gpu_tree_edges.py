@@ -113,7 +113,8 @@ def test_vocabularies_around_a_threads_share(mode, vocab):
 
 
 @pytest.mark.parametrize("mode", [sled.GREEDY, sled.SAMPLE], ids=["greedy", "sample"])
-@pytest.mark.parametrize("sizes", [[4] * 64, [4] * 63 + [5], [1] * 65, [16] * 128, [16] * 128 + [1], [64] * 64 + [3]], ids=lambda s: f"{len(s)}x{sum(s)}")
+@pytest.mark.parametrize("sizes", [[4] * 64, [4] * 63 + [5], [1] * 65, [16] * 64, [16] * 64 + [1], [32] * 48, [32] * 48 + [1], [16] * 128, [16] * 128 + [1], [64] * 64 + [3]],
+                         ids=lambda s: f"{len(s)}x{sum(s)}")
 def test_batches_around_the_sizes_that_travel_with_a_launch(mode, sizes):
     trees = [accept.random_tree(np.random.default_rng(i), n) for i, n in enumerate(sizes)]
     logits, tokens, u = accept.case(trees, 300, seed=len(sizes))
