@@ -13,6 +13,10 @@
 //                         by piece; into another request's pages pieces are independent and go to several workgroups.
 //                         K moves in 16-byte pieces (8 dims of a token); the V pages hold four tokens of a dim together, so V is gathered
 //                         value by value and written in 16 bytes.
+// What bounds it: memory.  A line of 128 bytes holds pieces of eight tokens (K) or four tokens of 16 dims (V), so with a third of the tokens kept most
+// lines are fetched whole: 8 requests of 27803 tokens in all cut to 1111 each, 32 layers of 8 heads of 128: 2.8 of 3.6 GB fetched and 1.1 written in
+// 800 us, 4.9 TB/s; the kept tokens alone would be 2.3 GB.  One request of 2048 tokens cut to 1024: 96 us for 0.4 GB.  Choosing takes 55 and 11 us
+// (five passes over a head's masses out of L2, bound by their latency).
 #include "sled_internal.h"
 
 #include <type_traits>

@@ -22,6 +22,14 @@
 //   writes them into the request's tail slots, which nobody reads in this launch.  Items of one (request, kv head, row group) store their
 //   states and the last to arrive adds them up in ascending order.
 //   fp32 models: the same with v_mfma_f32_16x16x4_f32 and single pages.
+// What bounds it: a step of 32 tokens costs a wavefront 24 matrix instructions, 85 vector ones and 8 exponentials.  On one SIMD matrix instructions hold
+// the port for 8 clocks, the others for 4 to 5 and exponentials for 9 (measured), so two wavefronts need 1200 clocks a step where 1650 are measured; the
+// rest is the wait at the step's barrier and for LDS.  16 requests (982 pages, 84 rows each, 8 kv heads) take 29 us a layer, 77 MB fetched
+// and 14 written; 64 requests (7204 pages, 139 rows each) 164 us with 566 to 592 MB fetched (472 without what second row groups read again) and
+// 66 written (27 of them results), 4.0 TB/s; one request of 300 tokens 9.9 us, a chain of launch, item, pages, three turns of LDS and
+// memory latency, merge.  Tried: DMA into LDS (a wavefront is held 200 clocks for each), wavefronts that read their own steps from memory (every row tile
+// of a wavefront costs registers, 128 rows need two: 200 us), K read a step early over a third LDS buffer (198 us), two steps between
+// barriers (188 us), all wavefronts in phase (174 us).
 // A value that is not finite must not reach the rows that do not see its node (0 * inf is NaN): such values of v are left out of the
 // product and added at the end for the rows that do see them.  Slots of the last context page behind L count as zero.
 #include "sled_internal.h"
@@ -774,6 +782,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_attention_kernel(tree_args
 // register and nothing but the last sum crosses lanes.  A wavefront holds MP pages of K in registers and walks through
 // the row tiles, whose operands all wavefronts of the workgroup share in LDS.  A token's sum is made by one
 // lane group in a fixed order: no atomics, and the same result every time.
+// What bounds it: 16 requests of 982 pages and 84 rows, 8 kv heads, take 16 us a layer, 7 of them K from memory, the walk 8; one request of 30011 tokens and
+// 512 rows 64 us, the walk 41 of them: a tile of 16 rows against 32 tokens holds a SIMD's port for 250 clocks (8 matrix instructions of 8 clocks,
+// 26 vector ones, 8 exponentials of 9) of 366 measured.  Four pages a wavefront leave room for one workgroup a CU: 18 and 79 us.
 constexpr int MASS_WAVES = 8;
 template <bool F32>
 __host__ __device__ constexpr int mass_pages() { return 2; }   // pages of a wavefront at a time
