@@ -1306,9 +1306,10 @@ size_t tree_plan_bytes(const sled_model* m, int B, int T, int64_t ctx_tokens) {
     const int Hkv = m->s.n_kv_heads, G = m->s.n_q_heads / Hkv;
     const int64_t n_pages = ctx_tokens / 16 + 2 * (int64_t)B, n_mass = Hkv * (n_pages / MASS_ITEM_PAGES + B);
     const int64_t groups = std::min<int64_t>((int64_t)B * ceil_div(SLED_TREE_MAX * G, GROUP), B + (int64_t)T * G / GROUP);
+    const int64_t each = std::min<int64_t>(ceil_div(SLED_TREE_MAX * G, GROUP), groups);   // of one request: the one with all the context, if need be
     // (runs of more than SLED_TREE_RUN pages are cut whatever the cap)
-    int64_t items = tree_item_cap(groups, Hkv) + ceil_div(n_pages, SLED_TREE_RUN / 2) * Hkv * ceil_div(groups, B);
-    if (m->batch_invariant) items = std::max(items, (ctx_tokens / (16 * SLED_FIXED_CHUNK_PAGES) + B) * Hkv * ceil_div(groups, B));
+    int64_t items = tree_item_cap(groups, Hkv) + (n_pages / (SLED_TREE_RUN / 2) + 1) * Hkv * each;
+    if (m->batch_invariant) items = std::max(items, (n_pages / SLED_FIXED_CHUNK_PAGES + 1) * Hkv * each + groups * Hkv);
     return tree_plan_layout(m, items, items * SLED_TREE_TILES, n_mass, T, n_pages).total;
 }
 

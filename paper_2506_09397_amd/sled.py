@@ -389,7 +389,7 @@ def sled_accept_tree(mode: int, n_nodes: Sequence[int], parents: Sequence[Sequen
     assert u is None or (u.dtype is floats and u.numel() == T)
     assert accept_len.dtype is ints and out_token.dtype is ints and path.dtype is ints and path.shape == (B, TREE_MAX)
     assert accept_len.numel() == out_token.numel() == B
-    _check(lib().sled_accept_tree(mode, B, _packed(n_nodes), _parents(n_nodes, parents), vocab, temperature, _ptr(logits), _ptr(tokens), _ptr(u),
+    _check(lib().sled_accept_tree(mode, B, _packed(n_nodes), _parents(n_nodes, parents), vocab, float(temperature), _ptr(logits), _ptr(tokens), _ptr(u),
                                   _ptr(accept_len), _ptr(path), _ptr(out_token), _ptr(workspace), _bytes(workspace), _stream()))
 
 

@@ -68,6 +68,18 @@ def test_contexts_longer_than_a_work_item_holds():
             assert bool(((b.out[0, at].double() - out).abs() <= tol).all()) and bool(((b.lse[0, at].double() - lse).abs() <= tol_lse).all())
 
 
+@pytest.mark.parametrize("invariant", [True, False])
+def test_the_workspace_asked_for_holds_one_large_tree_on_all_the_context(invariant):
+    """Several row groups on a long context, beside requests of one node: more items than an even share of groups would make."""
+    ctx, nodes = [31000] + [5] * 15, [64] + [1] * 15
+    with pool(*HEADS["70b"], n_pages=2000, invariant=invariant) as p:
+        b = Batch(p, ctx, nodes, seed=46)
+        b.run()
+        (out, lse, _, big, vmax), at = b.plain(0)
+        tol, tol_lse = attention_bounds(out, lse, big, vmax, 128, True)
+        assert bool(((b.out[0, at].double() - out).abs() <= tol).all()) and bool(((b.lse[0, at].double() - lse).abs() <= tol_lse).all())
+
+
 @pytest.mark.parametrize("heads", ["8b", "f32_64"])
 def test_lengths_that_the_host_does_not_know_yet(heads):
     """Trees begun right behind a commit: the host's bound counts every node as accepted, the length only those that were."""
