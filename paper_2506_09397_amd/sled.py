@@ -8,9 +8,10 @@ symbols fails loudly.
 """
 from __future__ import annotations
 
-import array
 import ctypes as C
+import itertools
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -304,19 +305,24 @@ def sled_profile_read(model: int):
 
 # ---------------------------------------------------------------------------------------- trees of drafts, eviction
 def _packed(xs: Sequence[int]):
-    a = array.array("i", xs)
-    return (C.c_int * len(a)).from_buffer(a)
+    return (C.c_int * len(xs)).from_buffer_copy(struct.pack(f"{len(xs)}i", *xs))
 
 
 def _parents(n_nodes: Sequence[int], parents: Sequence[Sequence[int]]):
     """parents[i][j]: the node that node j of tree i continues (parents[i][0] is not looked at), packed."""
-    assert len(parents) == len(n_nodes) and all(len(p) == n for p, n in zip(parents, n_nodes)), "a parent for every node of every tree"
-    flat = array.array("i")
-    for p in parents:
-        if len(p):
-            flat.append(-1)
-            flat.extend(p[1:])
-    return (C.c_int * len(flat)).from_buffer(flat)
+    assert list(map(len, parents)) == list(n_nodes), "a parent for every node of every tree"
+    T = sum(n_nodes)
+    try:
+        raw = struct.pack(f"{T}i", *itertools.chain.from_iterable(parents))
+    except struct.error:   # (roots may be anything)
+        raw = struct.pack(f"{T}i", *(x if j else -1 for p in parents for j, x in enumerate(p)))
+    flat = (C.c_int * T).from_buffer_copy(raw)
+    at = 0
+    for n in n_nodes:
+        if n:
+            flat[at] = -1
+        at += n
+    return flat
 
 
 def _rows(t: torch.Tensor, shape: Sequence[int]):
