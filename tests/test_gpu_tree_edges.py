@@ -131,3 +131,58 @@ def test_batches_around_the_sizes_that_travel_with_a_launch(mode, sizes):
     trees = [accept.random_tree(np.random.default_rng(i), n) for i, n in enumerate(sizes)]
     logits, tokens, u = accept.case(trees, 300, seed=len(sizes))
     accept.check(mode, trees, logits, tokens, u, temperature=1.25)
+
+
+@pytest.mark.parametrize("hq,D,dtype", [(32, 128, "bf16"), (16, 64, "f32")])
+def test_all_query_heads_on_one_kv_head(hq, D, dtype):
+    with pool(hq, 1, D, dtype, n_pages=200) as p:
+        b = Batch(p, [0, 77, 1000, 18], [1, 64, 9, 33], seed=47)
+        b.run()
+        b.check()
+        mass = torch.zeros(16, 1, 1, 1100, device="cuda")
+        sled.sled_tree_mass(p.pool, 0, b.q[0], b.lse[0], mass, b.ws)
+        torch.cuda.synchronize()
+        for i, (L, n) in enumerate(zip(b.ctx, b.n)):
+            m, off = mass_of(b, i)
+            assert bool(((mass[b.reqs[i], 0, :, :L + n].double() - m).abs() <= off).all())
+
+
+def test_two_pools_at_once():
+    """Attention, mass and acceptance of two pools on two streams, nothing waiting for anything: the same bits as one after the other."""
+    with pool(32, 8, 128, "bf16", layers=2, n_pages=600) as p0, pool(8, 2, 128, "f32", layers=2, n_pages=600) as p1:
+        batches = [Batch(p0, [900, 33, 2000], [40, 64, 7], seed=48, layers=2), Batch(p1, [1500, 0, 260], [9, 30, 64], seed=49, layers=2)]
+        walks = []
+        for k, vocab in enumerate((50000, 3001)):
+            trees = batches[k].trees
+            logits, tokens, u = accept.case(trees, vocab, seed=50 + k)
+            B, T = len(trees), sum(batches[k].n)
+            walks.append((trees, vocab, logits, tokens, u, sled.workspace(sled.sled_accept_tree_workspace_bytes(B, T, vocab)),
+                          *(torch.zeros(B, dtype=torch.int32, device="cuda") for _ in range(2)), torch.zeros(B, sled.TREE_MAX, dtype=torch.int32, device="cuda")))
+        mass = [torch.zeros(16, 2, b.p.shape.n_kv_heads, 2100, device="cuda") for b in batches]
+
+        def step(k):
+            b, (trees, vocab, logits, tokens, u, ws, a, o, path) = batches[k], walks[k]
+            sled.sled_tree_begin(b.p.pool, b.reqs, b.n, b.trees, b.ws)
+            for l in range(2):
+                sled.sled_tree_attention(b.p.pool, l, b.q[l], b.k[l], b.v[l], b.out[l], b.lse[l], b.ws)
+                sled.sled_tree_mass(b.p.pool, l, b.q[l], b.lse[l], mass[k], b.ws)
+            sled.sled_accept_tree(sled.SAMPLE if k else sled.GREEDY, b.n, trees, vocab, 0.9, logits, tokens, u, a, path, o, ws)
+
+        def results(k):
+            return [x.clone() for x in (batches[k].out, batches[k].lse, mass[k], *walks[k][6:])]
+
+        for k in range(2):
+            step(k)
+        torch.cuda.synchronize()
+        want = [results(k) for k in range(2)]
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        for _ in range(4):
+            for k in range(2):
+                batches[k].out.zero_(), batches[k].lse.zero_(), mass[k].zero_(), walks[k][8].zero_()
+            torch.cuda.synchronize()
+            for k in range(2):
+                with torch.cuda.stream(streams[k]):
+                    step(k)
+            torch.cuda.synchronize()
+            for k in range(2):
+                assert all(torch.equal(x, y) for x, y in zip(results(k), want[k]))
