@@ -6,7 +6,7 @@
 // the request stays one length and one page list while every head keeps its own tokens.
 //
 //   evict_select_kernel   a workgroup per (layer, kv head) and request.  The smallest mass that is kept is found digit by digit: four passes over
-//                         the masses, which L2 holds, each counting one byte of the values that agree so far with the bytes already known
+//                         the masses, in registers (beyond 8192 tokens in L2), each counting one byte of the values that agree so far with the bytes already known
 //                         in a histogram in LDS.  A last pass in ascending order gives every kept token its rank.
 //   evict_move_kernel     a workgroup per (layer, kv head), request and run of 64-token pieces.  A token of rank i moves down or stays (its
 //                         position is at least i), so a workgroup that reads a piece's 64 tokens before it writes them may work in place, piece
@@ -15,15 +15,15 @@
 //                         value by value and written in 16 bytes.
 // What bounds it: memory.  A line of 128 bytes holds pieces of eight tokens (K) or four tokens of 16 dims (V), so with a third of the tokens kept most
 // lines are fetched whole: 8 requests of 27803 tokens in all cut to 1111 each, 32 layers of 8 heads of 128: 2.8 of 3.6 GB fetched and 1.1 written in
-// 800 us, 4.9 TB/s; the kept tokens alone would be 2.3 GB.  One request of 2048 tokens cut to 1024: 96 us for 0.4 GB.  Choosing takes 55 and 11 us
-// (five passes over a head's masses out of L2, bound by their latency).
+// 800 us, 4.9 TB/s; the kept tokens alone would be 2.3 GB.  One request of 2048 tokens cut to 1024: 96 us for 0.4 GB.  Choosing takes 44 and 9 us
+// (55 and 12 with each pass over the masses out of L2).
 #include "sled_internal.h"
 
 #include <type_traits>
 
 namespace {
 
-constexpr int SEL_THREADS = 512, PIECE = 64;   // tokens of a piece: four pages
+constexpr int SEL_THREADS = 512, HELD = 16, PIECE = 64;   // masses that a thread holds; tokens of a piece: four pages
 
 // orders like the float, as an unsigned number (+0 and -0 alike)
 __device__ inline uint32_t order_key(float x) {
@@ -54,6 +54,10 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(evict_args a)
     const float* m = a.mass + (src * n_lh + lh) * a.cap;
     float* out = a.mass + (dst * n_lh + lh) * a.cap;
     int32_t* idx = a.idx + (b * n_lh + lh) * a.idx_cap;
+    if (src != dst && lh == 0 && tid == 0) {   // (nobody reads the destination's length in this call)
+        a.shift_dev[dst] = a.shift_dev[src] + L - keep;
+        a.len_dev[dst] = keep;
+    }
     if (keep == L) {   // everything stays
         if (src == dst) return;
         for (int i = tid; i < L; i += SEL_THREADS) {
@@ -61,6 +65,16 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(evict_args a)
             out[i] = m[i];
         }
         return;
+    }
+    // up to 8192 tokens: read once, and all at a time
+    const bool held = L <= HELD * SEL_THREADS;
+    float x[HELD];
+    if (held) {
+#pragma unroll
+        for (int r = 0; r < HELD; r++) {
+            if (r * SEL_THREADS >= L) break;
+            x[r] = m[min(r * SEL_THREADS + tid, L - 1)];
+        }
     }
     const int lo = a.first, hi = L - a.recent;   // the positions to choose from; more of them than are wanted, since keep < L
     const uint32_t want = keep - a.first - a.recent;
@@ -70,9 +84,19 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(evict_args a)
             for (int i = tid; i < 256; i += SEL_THREADS) hist[i] = 0;
             __syncthreads();
             const uint32_t known = shift == 24 ? 0u : ~0u << (shift + 8);
-            for (int i = lo + tid; i < hi; i += SEL_THREADS) {
-                const uint32_t k = order_key(m[i]);
+            auto count = [&](float v) {
+                const uint32_t k = order_key(v);
                 if ((k & known) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+            };
+            if (held) {
+#pragma unroll
+                for (int r = 0; r < HELD; r++) {
+                    if (r * SEL_THREADS >= hi) break;
+                    const int i = r * SEL_THREADS + tid;
+                    if (i >= lo && i < hi) count(x[r]);
+                }
+            } else {
+                for (int i = lo + tid; i < hi; i += SEL_THREADS) count(m[i]);
             }
             __syncthreads();
             if (wave == 0) {
@@ -102,11 +126,10 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(evict_args a)
     }
     // ranks, 512 positions at a time: kept are keys above the prefix and the first `left` of those equal to it
     int n_kept = 0, n_eq = 0;
-    for (int i0 = 0; i0 < L; i0 += SEL_THREADS) {
-        const int i = i0 + tid;
-        const float x = i < L ? m[i] : 0.f;
+    auto place = [&](int i, float v) {
+        asm volatile("" : : "v"(v));   // (it has arrived before the barriers behind which it may be overwritten)
         const bool mid = i >= lo && i < hi;
-        const uint32_t k = order_key(x);
+        const uint32_t k = order_key(v);
         const bool eq = mid && want > 0 && k == prefix;
         const uint64_t eqs = __ballot(eq), below = (1ull << lane) - 1ull;
         if (lane == 0) sh_eq[wave] = __popcll(eqs);
@@ -129,10 +152,19 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(evict_args a)
         }
         if (kept) {
             idx[rank] = i;
-            out[rank] = x;
+            out[rank] = v;
         }
         n_eq += all_eq;
         n_kept += all;
+    };
+    if (held) {
+#pragma unroll
+        for (int r = 0; r < HELD; r++) {
+            if (r * SEL_THREADS >= L) break;
+            place(r * SEL_THREADS + tid, x[r]);
+        }
+    } else {
+        for (int i0 = 0; i0 < L; i0 += SEL_THREADS) place(i0 + tid, i0 + tid < L ? m[i0 + tid] : 0.f);
     }
     __syncthreads();
     for (int i = keep + tid; i < L; i += SEL_THREADS) out[i] = 0.f;
@@ -220,7 +252,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(evict_args a) {
     }
 }
 
-// lengths after an eviction; the tokens to come keep the positions they would have had
+// lengths after an eviction in place (the choice sets those of other destinations); the tokens to come keep the positions they would have had
 __global__ void evict_len_kernel(evict_args a, int B) {
     const int b = blockIdx.x * blockDim.x + threadIdx.x;
     if (b >= B) return;
@@ -352,8 +384,10 @@ int sled_launch_evict(const sled_model* m, const sled_kvpool* p, const int32_t* 
     if (s.dtype == SLED_BF16) rc = launch_move<128, false>(a, B, in_place, split, st);
     else rc = s.head_dim == 64 ? launch_move<64, true>(a, B, in_place, split, st) : launch_move<128, true>(a, B, in_place, split, st);
     if (rc != SLED_OK) return rc;
-    hipLaunchKernelGGL(evict_len_kernel, dim3((B + 63) / 64), dim3(64), 0, st, a, B);
-    SLED_LAUNCH_CHECK();
+    if (in_place) {
+        hipLaunchKernelGGL(evict_len_kernel, dim3((B + 63) / 64), dim3(64), 0, st, a, B);
+        SLED_LAUNCH_CHECK();
+    }
     return SLED_OK;
 }
 

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import test_gpu_accept_tree as accept
+import test_gpu_evict as evict
 from paper_2506_09397_amd import sled
 from test_gpu_tree_attention import HEADS, Batch
 from tree_common import attention_bounds, generator, pool
@@ -186,3 +187,13 @@ def test_two_pools_at_once():
             torch.cuda.synchronize()
             for k in range(2):
                 assert all(torch.equal(x, y) for x, y in zip(results(k), want[k]))
+
+
+@pytest.mark.parametrize("fork", [False, True], ids=["in_place", "fork"])
+@pytest.mark.parametrize("kind", ["random", "ties"])
+def test_evictions_around_what_a_workgroup_holds(kind, fork):
+    """Up to 8192 masses stay in registers while the kept ones are chosen; nothing to choose between the first and the last."""
+    with pool(2, 2, 128, "bf16", n_pages=4500) as p:
+        evict.check_eviction(p, [8191, 8192, 8193, 9000], [4000, 8191, 200, 8999], 5, 100, kind, fork, seed=51)
+    with pool(2, 2, 128, "bf16", n_pages=2500) as p:
+        evict.check_eviction(p, [8192, 8195, 600], [300, 300, 300], 100, 200, kind, fork, seed=52)
