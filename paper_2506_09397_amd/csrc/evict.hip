@@ -11,17 +11,20 @@
 //   evict_move_kernel     a workgroup per (layer, kv head), request and run of 64-token pieces.  A token of rank i moves down or stays (its
 //                         position is at least i), so a workgroup that reads a piece's 64 tokens before it writes them may work in place, piece
 //                         by piece; into another request's pages pieces are independent and go to several workgroups.
-//                         K moves in 16-byte pieces (8 dims of a token); the V pages hold four tokens of a dim together, so V is gathered
-//                         value by value and written in 16 bytes.
+//                         K moves in 16-byte pieces (8 dims of a token); the V pages hold four tokens of a dim together, so every V value is
+//                         picked from the 16 bytes that its quad has of two dims, and four tokens are written together.
 // What bounds it: memory.  A line of 128 bytes holds pieces of eight tokens (K) or four tokens of 16 dims (V), so with a third of the tokens kept most
 // lines are fetched whole: 8 requests of 27803 tokens in all cut to 1111 each, 32 layers of 8 heads of 128: 2.8 of 3.6 GB fetched and 1.1 written in
-// 800 us, 4.9 TB/s; the kept tokens alone would be 2.3 GB.  One request of 2048 tokens cut to 1024: 96 us for 0.4 GB.  Choosing takes 44 and 9 us
+// 789 us, 5.0 TB/s; the kept tokens alone would be 2.3 GB.  One request of 2048 tokens cut to 1024: 85 us for 0.4 GB (96 with two loads of 2 bytes
+// for each value of V in place of one of 16).  Choosing takes 44 and 9 us
 // (55 and 12 with each pass over the masses out of L2).
 #include "sled_internal.h"
 
 #include <type_traits>
 
 namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int SEL_THREADS = 512, HELD = 16, PIECE = 64;   // masses that a thread holds; tokens of a piece: four pages
 
@@ -200,20 +203,17 @@ __global__ __launch_bounds__(256) void evict_move_kernel(evict_args a) {
         }
         __syncthreads();
         if constexpr (!F32) {
-            uint4 k[4];
-            bf16_t v[4][8];
+            // K: 16 bytes of token e16 of the page; V: four tokens (quad q4) of two dims, each out of the 16 bytes that its own quad has of them
+            u32x4 k[4], v[4][4];
             const int c4 = tid >> 6, q4 = (tid >> 4) & 3, e16 = tid & 15;
 #pragma unroll
             for (int p = 0; p < 4; p++) {
                 if (p * 16 >= n) break;
-                // K: 16 bytes of token e16 of the page; V: four tokens (quad q4) of two dims
-                k[p] = *reinterpret_cast<const uint4*>(kp + sh_at[p * 16 + e16] + (c4 * 64 + q4 * 16 + sh_slot[p * 16 + e16]) * 8);
+                k[p] = *reinterpret_cast<const u32x4*>(kp + sh_at[p * 16 + e16] + (c4 * 64 + q4 * 16 + sh_slot[p * 16 + e16]) * 8);
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    const int s = sh_slot[p * 16 + q4 * 4 + i];
-                    const bf16_t* x = vp + sh_at[p * 16 + q4 * 4 + i] + (c4 * 64 + (s >> 2) * 16 + e16) * 8 + (s & 3);
-                    v[p][i] = x[0];
-                    v[p][4 + i] = x[4];
+                    const int t = p * 16 + q4 * 4 + i;
+                    v[p][i] = *reinterpret_cast<const u32x4*>(vp + sh_at[t] + (c4 * 64 + (sh_slot[t] >> 2) * 16 + e16) * 8);
                 }
             }
             if (INPLACE) arrived();
@@ -221,23 +221,25 @@ __global__ __launch_bounds__(256) void evict_move_kernel(evict_args a) {
             for (int p = 0; p < 4; p++) {
                 if (p * 16 >= n) break;
                 const size_t d = at(to, (i0 >> 4) + p) + (size_t)tid * 8;
-                *reinterpret_cast<uint4*>(kp + d) = k[p];
-                uint4 w;
-                w.x = (uint32_t)v[p][0] | ((uint32_t)v[p][1] << 16);
-                w.y = (uint32_t)v[p][2] | ((uint32_t)v[p][3] << 16);
-                w.z = (uint32_t)v[p][4] | ((uint32_t)v[p][5] << 16);
-                w.w = (uint32_t)v[p][6] | ((uint32_t)v[p][7] << 16);
-                *reinterpret_cast<uint4*>(vp + d) = w;
+                *reinterpret_cast<u32x4*>(kp + d) = k[p];
+                uint32_t x[4][2];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int s = sh_slot[p * 16 + q4 * 4 + i], half = (s & 1) * 16;
+                    x[i][0] = (((s & 2) ? v[p][i][1] : v[p][i][0]) >> half) & 0xffffu;
+                    x[i][1] = (((s & 2) ? v[p][i][3] : v[p][i][2]) >> half) & 0xffffu;
+                }
+                *reinterpret_cast<u32x4*>(vp + d) = u32x4{x[0][0] | (x[1][0] << 16), x[2][0] | (x[3][0] << 16), x[0][1] | (x[1][1] << 16), x[2][1] | (x[3][1] << 16)};
             }
         } else {
             constexpr int CH = D / 4, N = PIECE * CH / 256;   // 16-byte pieces of a token; of this thread
-            float4 k[N], v[N];
+            u32x4 k[N], v[N];
 #pragma unroll
             for (int u = 0; u < N; u++) {
                 const int e = u * 256 + tid, t = e / CH, c = e % CH;
                 const size_t x = sh_at[t] + sh_slot[t] * D + c * 4;
-                k[u] = *reinterpret_cast<const float4*>(kp + x);
-                v[u] = *reinterpret_cast<const float4*>(vp + x);
+                k[u] = *reinterpret_cast<const u32x4*>(kp + x);
+                v[u] = *reinterpret_cast<const u32x4*>(vp + x);
             }
             if (INPLACE) arrived();
 #pragma unroll
@@ -245,8 +247,8 @@ __global__ __launch_bounds__(256) void evict_move_kernel(evict_args a) {
                 const int e = u * 256 + tid, t = e / CH, c = e % CH;
                 if (t >= n) continue;
                 const size_t x = at(to, (i0 + t) >> 4) + ((i0 + t) & 15) * D + c * 4;
-                *reinterpret_cast<float4*>(kp + x) = k[u];
-                *reinterpret_cast<float4*>(vp + x) = v[u];
+                *reinterpret_cast<u32x4*>(kp + x) = k[u];
+                *reinterpret_cast<u32x4*>(vp + x) = v[u];
             }
         }
     }
