@@ -406,7 +406,7 @@ __device__ __forceinline__ void attend_item(const tree_args& a, const int32_t* r
     const int32_t* pages = a.t.pages + rec[6];
     for (int i = tid; i < max(npg, 1); i += 64 * WAVES) sh.pages[i] = pages[page0 + i];   // (without context: the tail's page)
     const int L = a.len_dev[req];
-    const int G = a.Hq / a.Hkv, rows = G * n;
+    const int G = a.Hq / a.Hkv;
     const int rw = wave % NR, tg = wave / NR, lr = lane & 15, lg = lane >> 4;
     const bool mine = rw < n_tiles;   // this wavefront has a tile
     const size_t head = (size_t)16 * D, layer_page = (size_t)a.layer * a.n_pages;
