@@ -545,7 +545,8 @@ def main() -> None:
         # over workgroups, and a K/V value next to a bf16 rounding boundary can then land on its other side;
         # where the two best logits are closer than that, the argmax differs and the text takes another path
         # from there on (the drafter keeps proposing the old one, so that device's acceptance drops).
-        print("note: some devices left the precomputed continuation and were stopped there (near-ties of the two best logits)")
+        why = "their caches were cut" if args.kv_budget else "near-ties of the two best logits"
+        print(f"note: some devices left the precomputed continuation and were stopped there ({why})")
 
 
 if __name__ == "__main__":
