@@ -77,7 +77,7 @@ def check(mode, trees, logits, tokens, u, temperature=1.0):
 
 
 SIZES = [
-    # (trees' sizes, vocabulary): few rows (all scanned at once), many rows (step by step), odd and small vocabularies, one piece and several
+    # (trees' sizes, vocabulary): few rows (all scanned first), many rows (a workgroup goes through those of its walk), odd and small vocabularies, one piece and several
     ([1], 2), ([1], 128256), ([9], 128256), ([64], 50257), ([5, 1, 64, 17], 4099), ([32] * 16, 128256), ([3, 64, 40, 1] * 10, 32001), ([64] * 8, 128256),
     ([2, 7] * 60, 1000), ([1] * 1024, 37), ([64, 64, 64, 64, 64, 64, 64, 64] * 10, 257),
 ]
@@ -180,7 +180,7 @@ def test_draws_follow_the_targets_distribution():
 
 
 @pytest.mark.parametrize("mode", [sled.GREEDY, sled.SAMPLE], ids=["greedy", "sample"])
-@pytest.mark.parametrize("sizes,vocab", [([9, 3], 30000), ([64] * 40, 32000)], ids=["rows", "levels"])
+@pytest.mark.parametrize("sizes,vocab", [([9, 3], 30000), ([64] * 40, 32000)], ids=["few_rows", "many_rows"])
 def test_captured_and_replayed(mode, sizes, vocab):
     trees = [random_tree(np.random.default_rng(1), n) for n in sizes]
     logits, tokens, u = case(trees, vocab, seed=1)

@@ -100,7 +100,7 @@ def test_long_contexts_are_split_and_joined(heads, L):
 
 @pytest.mark.parametrize("heads,requests,L", [("g1", 256, 4200), ("f32_64", 128, 4801)])
 def test_more_than_one_block_of_page_numbers(heads, requests, L):
-    """A wavefront holds the numbers of 64 of its pages at a time; so many requests that a context is one work item of more pages than four times that."""
+    """So many requests that a context is one work item or a few, of hundreds of pages."""
     with pool(*HEADS[heads], n_pages=requests * ((L + 15) // 16 + 1), max_requests=requests) as p:
         b = Batch(p, [L] * requests, [1] * requests, seed=12)
         b.n, b.trees = [1] * requests, [[-1]] * requests
