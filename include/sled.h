@@ -427,7 +427,8 @@ SLED_API int sled_verify_tree(sled_model* m, sled_kvpool* p, int B, const int* r
  *   u[T]                   dev float32 uniforms in [0, 1), one per node (SLED_SAMPLE only, else may be NULL)
  *   accept_len[B]          dev int32 out: accepted drafts;  out_token[B]  dev int32 out: the token that follows them
  *   path[B][SLED_TREE_MAX] dev int32 out: the accepted nodes in order, -1 behind them
- *   workspace              dev scratch of at least sled_accept_tree_workspace_bytes(B, T, vocab) bytes, 256-byte aligned
+ *   workspace              dev scratch of at least sled_accept_tree_workspace_bytes(B, T, vocab) bytes, 256-byte aligned (what
+ *                          is enough for B and T is enough for smaller ones)
  * Allocates nothing and can be captured (the trees' shape is part of the captured launch).  B <= 1024.  Errors: SLED_EINVAL. */
 SLED_API size_t sled_accept_tree_workspace_bytes(int B, int T, int vocab);
 SLED_API int sled_accept_tree(int mode, int B, const int* n_nodes /*host*/, const int* parent /*host*/, int vocab, float temperature,

@@ -459,8 +459,10 @@ int pieces_of(int V) { return (V + seg_of(V) - 1) / seg_of(V); }
 
 }  // namespace
 
+// Grows with B and T: a call of more rows than are scanned has no use for their pieces, but a workspace for it also serves the smaller ones that have.
 size_t sled_accept_tree_ws_bytes(int B, int T, int vocab) {
-    const size_t part = scan_first(true, T, vocab) ? (size_t)T * pieces_of(vocab) * sizeof(Piece) : 0;
+    const int scanned = std::min(T, SCAN_ROWS_SAMPLE);
+    const size_t part = scan_first(true, scanned, vocab) ? (size_t)scanned * pieces_of(vocab) * sizeof(Piece) : 0;
     return up(part) + up((size_t)(B + 1) * 4) + up(T);
 }
 

@@ -1,0 +1,43 @@
+"""Tree operators called with workspaces that were sized for something larger."""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_accept_tree as accept
+from paper_2506_09397_amd import sled, synth
+from paper_2506_09397_amd.runtime import Verifier
+from tree_common import random_tree
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("mode", [sled.GREEDY, sled.SAMPLE], ids=["greedy", "sample"])
+def test_acceptance_with_a_workspace_for_the_largest_batch(mode):
+    V, nodes = 20011, 64
+    ws = sled.workspace(sled.sled_accept_tree_workspace_bytes(32, 32 * nodes, V))
+    for sizes in ([1], [9], [49] * 31, [48] * 32, [49] * 32, [64] * 32):      # 1536 rows are scanned first when sampling, 1568 are not
+        trees = [random_tree(np.random.default_rng(i), n) for i, n in enumerate(sizes)]
+        logits, tokens, u = accept.case(trees, V, seed=len(sizes))
+        ws.random_(0, 255)
+        got = [x.cpu().numpy() for x in accept.run(mode, trees, logits, tokens, u, 0.75, ws=ws)]
+        want, margin = accept.walk(mode, trees, logits.cpu().numpy(), tokens.cpu().numpy(), u.cpu().numpy(), 0.75)
+        assert margin > 1e-12
+        assert [(int(a), p.tolist(), int(t)) for a, p, t in zip(*got)] == want
+
+
+def test_a_verifier_for_many_large_trees_accepts_small_batches():
+    """Room for 32 trees of 64 nodes, steps of one tree and of a few."""
+    shape = synth.SHAPES["tiny_bf16"]
+    v = Verifier(shape, synth.SynthWeights(shape, seed=1, device="cuda"), 400, 32, 32, 4000)
+    v.enable_trees(64, 2000)
+    rng = np.random.default_rng(2)
+    reqs = [v.open() for _ in range(5)]
+    for B in (1, 5):
+        trees = [random_tree(rng, n) for n in (3, 64, 63, 9, 33)[:B]]
+        tokens = torch.from_numpy(rng.integers(0, shape.vocab, size=sum(map(len, trees))).astype(np.int32)).cuda()
+        logits = v.verify_tree(reqs[:B], trees, tokens)
+        a, path, t = v.accept_tree(sled.GREEDY, trees, logits, tokens)
+        v.commit_tree(reqs[:B], a, path)
+        want, _ = accept.walk(sled.GREEDY, trees, logits.cpu().numpy(), tokens.cpu().numpy(), None, 1.0)
+        assert [(int(x), p, int(y)) for x, p, y in zip(a.tolist(), path.tolist(), t.tolist())] == want
+    v.destroy()
