@@ -83,8 +83,10 @@ __device__ inline int four_of(const float* __restrict__ row, int V, int j, Four&
     return 0;
 }
 
-// e^y for y <= 0 (NaN stays one): y = k ln 2 + r, the Taylor series of e^r up to r^11 (|r| <= ln 2 / 2: the rest is below 7e-15 of it)
+// e^y for y <= 0, zero for NaN: y = k ln 2 + r, the Taylor series of e^r up to r^11 (|r| <= ln 2 / 2: the rest is below 9e-15 of it).  Below -746 it is zero in
+// float64, and far below (a mask of the type's lowest value) k ln 2 would not be exact and r no longer small.
 __device__ inline double exp_below(double y) {
+    y = fmax(y, -746.0);
     const double k = rint(y * 1.4426950408889634);
     // ln 2 = 2977044471 / 2^32 + 1.908e-10: the first part times k is exact
     const double r = fma(-k, 1.9082149292705877e-10, fma(-k, 2977044471.0 / 4294967296.0, y));
@@ -100,13 +102,10 @@ __device__ inline double exp_below(double y) {
     e = fma(e, r, 0.5);
     e = fma(e, r, 1.0);
     e = fma(e, r, 1.0);
-    return ldexp(e, (int)fmax(k, -1100.0));
+    return ldexp(e, (int)k);
 }
 // weight of a value; one that is not a number, or lies as far above as infinity, has none
-__device__ inline double weight(float x, double m, double inv_tau) {
-    const double e = exp_below(((double)x - m) * inv_tau);
-    return e > 0.0 ? e : 0.0;
-}
+__device__ inline double weight(float x, double m, double inv_tau) { return exp_below(((double)x - m) * inv_tau); }
 
 struct walk_shared {
     float m[WAVES];
