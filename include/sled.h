@@ -377,7 +377,7 @@ SLED_API int sled_tree_begin(sled_kvpool* p, int B, const int* req_ids /*host*/,
  * Softmax and sums in float32; a bf16 model's weights enter the product with V with 16 significant bits, the result is
  * rounded once.  Keys and values of a node do not reach nodes that do not see it, not even where they are not finite.
  * out and lse must not overlap the inputs.  Results do not depend on the other requests of the batch but for the order of float32 sums over split contexts
- * (not even that for batch-invariant models).  Errors: SLED_EINVAL, SLED_ESTATE (no plan). */
+ * (not even that for batch-invariant models, nor whether the exact lengths of an earlier commit have arrived).  Errors: SLED_EINVAL, SLED_ESTATE (no plan). */
 SLED_API int sled_tree_attention(sled_kvpool* p, int layer, const void* q /*dev*/, int64_t q_stride, const void* k /*dev*/, int64_t k_stride,
                         const void* v /*dev*/, int64_t v_stride, void* out /*dev out*/, float* lse /*dev out or NULL*/,
                         void* workspace /*dev*/, void* stream);

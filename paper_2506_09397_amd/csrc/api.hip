@@ -1309,7 +1309,7 @@ size_t tree_plan_bytes(const sled_model* m, int B, int T, int64_t ctx_tokens) {
     const int64_t each = std::min<int64_t>(ceil_div(SLED_TREE_MAX * G, GROUP), groups);   // of one request: the one with all the context, if need be
     // (runs of more than SLED_TREE_RUN pages are cut whatever the cap)
     int64_t items = tree_item_cap(groups, Hkv) + (n_pages / (SLED_TREE_RUN / 2) + 1) * Hkv * each;
-    if (m->batch_invariant) items = std::max(items, (n_pages / SLED_FIXED_CHUNK_PAGES + 1) * Hkv * each + groups * Hkv);
+    if (m->batch_invariant) items = std::max(items, (n_pages / SLED_FIXED_CHUNK_PAGES + 1) * Hkv * each + 2 * groups * Hkv);
     return tree_plan_layout(m, items, items * SLED_TREE_TILES, n_mass, T, n_pages).total;
 }
 
@@ -1406,10 +1406,13 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
     at_group[B] = (int)groups.size();
     const int tgt = m->batch_invariant ? 0 : tree_item_length(groups, Hkv, P);
     auto chunk_of = [&](const tree_group& x) { return m->batch_invariant ? SLED_FIXED_CHUNK_PAGES : tree_chunk(x, tgt, P); };
+    // Items of a group and kv head; the last has the tree.  Batch-invariant: an item of its own, and at least one for the context, since how many pages
+    // that has is a bound here, which depends on whether a commit's lengths have arrived.  Runs that turn out empty add exactly nothing.
+    auto runs_of = [&](const tree_group& x) { return std::max(1, ceil_div(x.pages, chunk_of(x))) + (m->batch_invariant ? 1 : 0); };
     int64_t n_items = 0, n_slots = 0, n_mass = 0, mass_chunk = MASS_ITEM_PAGES;
     while (n_pages * Hkv / mass_chunk > 8192) mass_chunk *= 2;
     for (const tree_group& x : groups) {
-        const int64_t items = (int64_t)Hkv * std::max(1, ceil_div(x.pages, chunk_of(x)));
+        const int64_t items = (int64_t)Hkv * runs_of(x);
         n_items += items;
         n_slots += items * x.waves;
     }
@@ -1442,10 +1445,11 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
     for (int i : by_length) {
         for (int k = at_group[i]; k < at_group[i + 1]; k++) {
             const tree_group& x = groups[k];
-            const int chunk = chunk_of(x), runs = std::max(1, ceil_div(np[i], chunk)), first = at;
+            const int chunk = chunk_of(x), runs = runs_of(x), first = at;
             for (int c = 0; c < runs; c++)
                 for (int g = 0; g < Hkv; g++, at++) {
-                    const int32_t rec[SLED_TREE_ITEM] = {req_ids[i], g, c * chunk, std::min(chunk, np[i] - c * chunk), n_nodes[i], row0[i], page_at[i],
+                    const int run = std::max(0, std::min(chunk, np[i] - c * chunk));   // (none where the tree has an item of its own)
+                    const int32_t rec[SLED_TREE_ITEM] = {req_ids[i], g, run ? c * chunk : 0, run, n_nodes[i], row0[i], page_at[i],
                                                          first + g, runs, Hkv, x.tile0 * 16, c == runs - 1, x.tiles, x.waves, slot + g * x.waves};
                     memcpy(item + (size_t)at * SLED_TREE_ITEM, rec, sizeof(rec));
                 }

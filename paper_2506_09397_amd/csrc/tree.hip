@@ -404,7 +404,7 @@ __device__ __forceinline__ void attend_item(const tree_args& a, const int32_t* r
     const bool last = rec[11] != 0;   // the item that has the tree
     const int n_tiles = rec[12], slot0 = rec[14];
     const int32_t* pages = a.t.pages + rec[6];
-    for (int i = tid; i < max(npg, 1); i += 64 * WAVES) sh.pages[i] = pages[page0 + i];   // (without context: the tail's page)
+    for (int i = tid; i < max(npg, 1); i += 64 * WAVES) sh.pages[i] = pages[page0 + i];   // (without context: the request's first page)
     const int L = a.len_dev[req];
     const int G = a.Hq / a.Hkv;
     const int rw = wave % NR, tg = wave / NR, lr = lane & 15, lg = lane >> 4;
