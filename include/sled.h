@@ -386,9 +386,13 @@ SLED_API int sled_tree_attention(sled_kvpool* p, int layer, const void* q /*dev*
  * heads of a kv head of softmax(q K^T / sqrt(head_dim))[token].  For sled_kv_evict.  Comes after sled_tree_attention of that layer,
  * with its q and the lse it returned.
  *   mass  dev float32 [max_requests][n_layers][n_kv_heads][mass_cap], the row of a request by its id; mass_cap at least the
- *         library's bound of L_i + n_i.  Zero a request's rows when it is opened; at and behind position L they are zero
- *         whenever no tree is staged.  A node's own slot gets its mass (set, not added to), which sled_tree_commit moves with the node.
- * One sum in a fixed order per token: no atomics.  Errors: SLED_EINVAL, SLED_ESTATE (no plan). */
+ *         library's bound of L_i + n_i; one array for a pool.  Zero a request's rows when it is opened.  A node's own slot gets its mass
+ *         (set, not added to), which sled_tree_commit, given the same array, moves with the node.  What the nodes of a tree that is dropped
+ *         have got stays in their slots until the next call on the request that is given mass (this one, sled_verify_tree, sled_tree_commit,
+ *         sled_kv_evict), which clears it first: tokens that come to lie there start from zero.  Otherwise entries at and behind position L are
+ *         zero whenever no tree is staged.
+ * One sum in a fixed order per token: no atomics.  Errors: SLED_EINVAL, SLED_ESTATE (no plan; captured while a dropped tree's mass waits to
+ * be cleared). */
 SLED_API int sled_tree_mass(sled_kvpool* p, int layer, const void* q /*dev*/, int64_t q_stride, const float* lse /*dev*/, float* mass /*dev inout*/,
                    int mass_cap, void* workspace /*dev*/, void* stream);
 

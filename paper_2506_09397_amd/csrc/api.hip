@@ -353,7 +353,7 @@ extern "C" int sled_kvpool_create(const sled_model* m, int64_t n_pages, int max_
     p->max_requests = max_requests;
     p->page_head_elems = (size_t)16 * m->s.head_dim;
     p->k_pool = p->v_pool = nullptr;
-    p->len_dev = p->shift_dev = nullptr;
+    p->len_dev = p->shift_dev = p->tail_dev = nullptr;
     for (int i = 0; i < sled_kvpool::RING; i++) p->slot[i] = sled_stage_slot{nullptr, nullptr, nullptr, false};
     p->stage_cap = 0;
     p->stage_next = 0;
@@ -370,11 +370,14 @@ extern "C" int sled_kvpool_create(const sled_model* m, int64_t n_pages, int max_
         return fail(SLED_ENOMEM, "hipMalloc(lengths)", e);
     if ((e = hipMalloc(reinterpret_cast<void**>(&p->shift_dev), max_requests * sizeof(int32_t))) != hipSuccess)
         return fail(SLED_ENOMEM, "hipMalloc(lengths)", e);
+    if ((e = hipMalloc(reinterpret_cast<void**>(&p->tail_dev), 2 * (size_t)max_requests * sizeof(int32_t))) != hipSuccess)
+        return fail(SLED_ENOMEM, "hipMalloc(lengths)", e);
     // pages never written hold zeros (read only under the mask, but keep them finite)
     if ((e = hipMemset(p->k_pool, 0, bytes)) != hipSuccess) return fail(SLED_EHIP, "hipMemset", e);
     if ((e = hipMemset(p->v_pool, 0, bytes)) != hipSuccess) return fail(SLED_EHIP, "hipMemset", e);
     if ((e = hipMemset(p->len_dev, 0, max_requests * sizeof(int32_t))) != hipSuccess) return fail(SLED_EHIP, "hipMemset", e);
     if ((e = hipMemset(p->shift_dev, 0, max_requests * sizeof(int32_t))) != hipSuccess) return fail(SLED_EHIP, "hipMemset", e);
+    if ((e = hipMemset(p->tail_dev, 0, 2 * (size_t)max_requests * sizeof(int32_t))) != hipSuccess) return fail(SLED_EHIP, "hipMemset", e);
     p->stage_cap = 1 << 16;
     for (int i = 0; i < sled_kvpool::RING; i++) {
         if (slot_alloc(p->slot[i], p->stage_cap) != SLED_OK) {
@@ -414,6 +417,7 @@ extern "C" int sled_kvpool_destroy(sled_kvpool* p) {
     if (p->v_pool) (void)hipFree(p->v_pool);
     if (p->len_dev) (void)hipFree(p->len_dev);
     if (p->shift_dev) (void)hipFree(p->shift_dev);
+    if (p->tail_dev) (void)hipFree(p->tail_dev);
     delete p;
     return SLED_OK;
 }
@@ -436,6 +440,12 @@ extern "C" int sled_kvpool_open(sled_kvpool* p, int* req_id) {
     SLED_FAIL(SLED_ENOMEM, "sled_kvpool_open: all %d request slots are in use", p->max_requests);
 }
 
+// A request's staged tree goes without a commit that knows its mass: what its nodes have got stays behind.
+static void drop_mass(sled_request& rq) {
+    rq.mass_left = rq.mass_left || rq.mass_added;
+    rq.mass_added = false;
+}
+
 // A request's length or pages change, or its tail slots are overwritten: the trees at hand cannot be attended to any more, and this request's
 // cannot be committed (the others' can).
 static void leave_tree(sled_kvpool* p, int req) {
@@ -444,6 +454,7 @@ static void leave_tree(sled_kvpool* p, int req) {
     if (it == t.reqs.end()) return;
     t.reqs.erase(it);
     t.valid = false;
+    drop_mass(p->reqs[req]);
 }
 
 extern "C" int sled_kvpool_close(sled_kvpool* p, int req_id) {
@@ -498,7 +509,7 @@ static int reset_fresh_lengths(sled_kvpool* p, int B, const int* req_ids, hipStr
     std::vector<int> ids;
     for (int i = 0; i < B; i++)
         if (p->reqs[req_ids[i]].fresh) ids.push_back(req_ids[i]);
-    const int rc = sled_launch_len_zero(p->len_dev, p->shift_dev, ids.data(), (int)ids.size(), st);
+    const int rc = sled_launch_len_zero(p, ids.data(), (int)ids.size(), st);
     if (rc != SLED_OK) return rc;
     for (int r : ids) p->reqs[r].fresh = false;
     return SLED_OK;
@@ -582,7 +593,7 @@ extern "C" int sled_kv_append(sled_kvpool* p, int B, const int* req_ids, const i
         if ((rc = stage_acquire(p, B, &sl)) != SLED_OK) return rc;
         for (int i = 0; i < B; i++) sl->host[i] = req_ids[i];
         SLED_HIP(hipMemcpyAsync(sl->dev, sl->host, B * sizeof(int32_t), hipMemcpyHostToDevice, st));
-        if ((rc = sled_launch_len_add(p->len_dev, p->shift_dev, sl->dev, nullptr, nullptr, accept_len, B, st)) != SLED_OK) return rc;
+        if ((rc = sled_launch_len_add(p, sl->dev, nullptr, nullptr, accept_len, B, st)) != SLED_OK) return rc;
         if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
         for (int i = 0; i < B; i++) {
             sled_request& rq = p->reqs[req_ids[i]];
@@ -620,7 +631,7 @@ extern "C" int sled_kv_append(sled_kvpool* p, int B, const int* req_ids, const i
     }
     SLED_HIP(hipMemcpyAsync(sl->dev, sl->host, off * sizeof(int32_t), hipMemcpyHostToDevice, st));
     if ((rc = sled_launch_kv_ingest(m, p, pieces.data(), (int)pieces.size(), st)) != SLED_OK) return rc;
-    if ((rc = sled_launch_len_add(p->len_dev, p->shift_dev, sl->dev, sl->dev + B, sl->dev + 2 * B, nullptr, B, st)) != SLED_OK) return rc;
+    if ((rc = sled_launch_len_add(p, sl->dev, sl->dev + B, sl->dev + 2 * B, nullptr, B, st)) != SLED_OK) return rc;
     if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
     for (int i = 0; i < B; i++) {
         sled_request& rq = p->reqs[req_ids[i]];
@@ -1168,7 +1179,7 @@ extern "C" int sled_prefill(sled_model* m, sled_kvpool* p, int req_id, int n_tok
         sl->host[0] = req_id;
         sl->host[1] = rows;
         SLED_HIP(hipMemcpyAsync(sl->dev, sl->host, 2 * sizeof(int32_t), hipMemcpyHostToDevice, st));
-        if ((rc = sled_launch_len_add(p->len_dev, p->shift_dev, sl->dev, sl->dev + 1, nullptr, nullptr, 1, st)) != SLED_OK) return rc;
+        if ((rc = sled_launch_len_add(p, sl->dev, sl->dev + 1, nullptr, nullptr, 1, st)) != SLED_OK) return rc;
         if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
         rq.len_ub += rows;
         rq.added += rows;
@@ -1478,7 +1489,10 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
     t.max_nodes = nmax;
     t.T = T;
     // what earlier steps staged for these requests is overwritten, and only the last trees can be committed
-    for (int r : p->tree.reqs) p->reqs[r].staged = -1;
+    for (int r : p->tree.reqs) {
+        p->reqs[r].staged = -1;
+        drop_mass(p->reqs[r]);
+    }
     for (int i = 0; i < B; i++) {
         p->last_batch.erase(std::remove(p->last_batch.begin(), p->last_batch.end(), req_ids[i]), p->last_batch.end());
         p->reqs[req_ids[i]].staged = n_nodes[i];
@@ -1506,6 +1520,27 @@ int check_mass(const sled_kvpool* p, int mass_cap, int reach, const char* who) {
         SLED_FAIL(SLED_EINVAL, "%s: mass rows of %d entries, but a request may reach %d tokens (sled_kvpool_lengths gives exact lengths to the library)", who,
                   mass_cap, reach);
     (void)p;
+    return SLED_OK;
+}
+
+// Before mass is read or added to: slots in which dropped nodes have left some are cleared.  staged: also those of the trees at hand, which go now.
+int clear_mass(sled_kvpool* p, int B, const int* req_ids, bool staged, float* mass, int mass_cap, hipStream_t st, const char* who) {
+    std::vector<int> ids;
+    for (int i = 0; i < B; i++) {
+        const sled_request& rq = p->reqs[req_ids[i]];
+        if (rq.mass_left || (staged && rq.mass_added)) ids.push_back(req_ids[i]);
+    }
+    if (ids.empty()) return SLED_OK;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    SLED_HIP(hipStreamIsCapturing(st, &status));
+    if (status != hipStreamCaptureStatusNone)
+        SLED_FAIL(SLED_ESTATE, "%s: a dropped tree has left mass, which cannot be cleared by a captured call (make one first that is not captured)", who);
+    int rc;
+    if ((rc = sled_launch_mass_clear(p->m, p, ids.data(), (int)ids.size(), mass, mass_cap, st)) != SLED_OK) return rc;
+    for (int r : ids) {
+        p->reqs[r].mass_left = false;
+        if (staged) p->reqs[r].mass_added = false;
+    }
     return SLED_OK;
 }
 
@@ -1566,7 +1601,7 @@ extern "C" int sled_tree_attention(sled_kvpool* p, int layer, const void* q, int
     return sled_launch_tree_attention(m, p, p->tree.plan, layer, q, q_stride, 0, k, k_stride, v, v_stride, out, 0, lse, false, static_cast<hipStream_t>(stream));
 }
 
-extern "C" int sled_tree_mass(sled_kvpool* p, int layer, const void* q, int64_t q_stride, const float* lse, float* mass, int mass_cap, void* workspace, void* stream) {
+extern "C" int sled_tree_mass(sled_kvpool* p, int layer, const void* q, int64_t q_stride, const float* lse, float* mass, int mass_cap, void* workspace, void* stream) try {
     if (!p || !lse || !mass) SLED_FAIL(SLED_EINVAL, "sled_tree_mass: null argument");
     if (!p->tree.valid) SLED_FAIL(SLED_ESTATE, "sled_tree_mass: no trees at hand (sled_tree_begin comes first)");
     const sled_model* m = p->m;
@@ -1575,8 +1610,12 @@ extern "C" int sled_tree_mass(sled_kvpool* p, int layer, const void* q, int64_t 
     int rc;
     if ((rc = check_rows(m, q, q_stride, m->s.n_q_heads * m->s.head_dim, "q", "sled_tree_mass")) != SLED_OK) return rc;
     if ((rc = check_mass(p, mass_cap, p->tree.max_reach, "sled_tree_mass")) != SLED_OK) return rc;
-    return sled_launch_tree_mass(m, p, p->tree.plan, layer, q, q_stride, 0, lse, mass, mass_cap, static_cast<hipStream_t>(stream));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if ((rc = clear_mass(p, (int)p->tree.reqs.size(), p->tree.reqs.data(), false, mass, mass_cap, st, "sled_tree_mass")) != SLED_OK) return rc;
+    for (int r : p->tree.reqs) p->reqs[r].mass_added = true;
+    return sled_launch_tree_mass(m, p, p->tree.plan, layer, q, q_stride, 0, lse, mass, mass_cap, st);
 }
+SLED_CATCH("sled_tree_mass")
 
 extern "C" int sled_tree_commit(sled_kvpool* p, int B, const int* req_ids, const int32_t* accept_len, const int32_t* path, float* mass, int mass_cap, void* stream) try {
     if (!p || !req_ids || !accept_len || !path) SLED_FAIL(SLED_EINVAL, "sled_tree_commit: null argument");
@@ -1593,6 +1632,7 @@ extern "C" int sled_tree_commit(sled_kvpool* p, int B, const int* req_ids, const
         if (mass && (rc = check_mass(p, mass_cap, rq.len_ub + rq.staged, "sled_tree_commit")) != SLED_OK) return rc;
         need += rq.pages.size();
     }
+    if (mass && (rc = clear_mass(p, B, req_ids, false, mass, mass_cap, st, "sled_tree_commit")) != SLED_OK) return rc;
     sled_stage_slot* sl;
     if ((rc = stage_acquire(p, need, &sl)) != SLED_OK) return rc;
     size_t off = 3 * (size_t)B;
@@ -1611,6 +1651,7 @@ extern "C" int sled_tree_commit(sled_kvpool* p, int B, const int* req_ids, const
         rq.len_ub += rq.staged;   // every node of a chain may have been accepted; the exact lengths follow
         rq.added += rq.staged;
         rq.staged = -1;
+        if (mass) rq.mass_added = false;
         leave_tree(p, req_ids[i]);
     }
     return enqueue_readback(p, B, req_ids, st);
@@ -1640,6 +1681,10 @@ extern "C" int sled_verify_tree(sled_model* m, sled_kvpool* p, int B, const int*
     char* ws = static_cast<char*>(workspace);
     if ((rc = plan_trees(p, B, req_ids, n_nodes, parent, ws + w.plan, workspace_bytes - w.plan, st, "sled_verify_tree")) != SLED_OK) return rc;
     p->tree.valid = false;   // (the plan serves this step alone; the nodes stay staged for the commit)
+    if (mass) {
+        if ((rc = clear_mass(p, B, req_ids, false, mass, mass_cap, st, "sled_verify_tree")) != SLED_OK) return rc;
+        for (int i = 0; i < B; i++) p->reqs[req_ids[i]].mass_added = true;
+    }
     std::vector<step_entry> ent(B);
     for (int i = 0; i < B; i++) ent[i] = step_entry{req_ids[i], 0, n_nodes[i]};
     const tree_step tr{&p->tree.plan, depth.data(), ws + w.k, ws + w.v, reinterpret_cast<float*>(ws + w.lse), mass, mass_cap};
@@ -1707,6 +1752,8 @@ extern "C" int sled_kv_evict(sled_kvpool* p, int B, const int* req_ids, const in
     if (idx_bytes > workspace_bytes) SLED_FAIL(SLED_EINVAL, "sled_kv_evict: workspace of %zu bytes, %zu needed", workspace_bytes, idx_bytes);
     if ((rc = reset_fresh_lengths(p, B, req_ids, st)) != SLED_OK) return rc;
     if (!in_place && (rc = reset_fresh_lengths(p, B, dst_ids, st)) != SLED_OK) return rc;
+    if ((rc = clear_mass(p, B, req_ids, in_place, mass, mass_cap, st, "sled_kv_evict")) != SLED_OK) return rc;
+    if (!in_place && (rc = clear_mass(p, B, dst_ids, false, mass, mass_cap, st, "sled_kv_evict")) != SLED_OK) return rc;
     size_t need = (size_t)SLED_EVICT_REC * B;
     for (int i = 0; i < B; i++) {
         const int src_ub = p->reqs[req_ids[i]].len_ub;

@@ -280,6 +280,7 @@ struct commit_args {
     int32_t* len_dev;
     const int32_t *accept_len, *path;   // [B], [B][SLED_TREE_MAX]
     float* mass;                        // or nullptr
+    int32_t* tail;                      // with mass: where nodes have some
     int cap, n_layers, Hkv, D;
     void *k_pool, *v_pool;
     int64_t n_pages;
@@ -360,6 +361,15 @@ __global__ __launch_bounds__(64) void tree_len_kernel(commit_args a) {
     int node;
     const int len = path_length(a.path + (size_t)b * SLED_TREE_MAX, a.accept_len[b], rec[1], lane, &node);
     if (lane == 0) a.len_dev[rec[0]] += len + 1;
+    if (a.mass && lane < 2) a.tail[2 * rec[0] + lane] = 0;
+}
+
+// What nodes that were dropped have left behind, a workgroup per request: up to 64 slots of every layer and head.
+__global__ __launch_bounds__(256) void mass_clear_kernel(sled_some_ids ids, int32_t* __restrict__ tail, float* __restrict__ mass, int cap, int n_lh) {
+    const int r = ids.id[blockIdx.x], from = tail[2 * r], n = min(tail[2 * r + 1], cap) - from;
+    for (int i = threadIdx.x; i < n_lh * n; i += 256) mass[((size_t)r * n_lh + i / n) * cap + from + i % n] = 0.f;
+    __syncthreads();
+    if (threadIdx.x < 2) tail[2 * r + threadIdx.x] = 0;
 }
 
 template <int D, bool F32>
@@ -393,10 +403,21 @@ int sled_launch_evict(const sled_model* m, const sled_kvpool* p, const int32_t* 
     return SLED_OK;
 }
 
+int sled_launch_mass_clear(const sled_model* m, const sled_kvpool* p, const int* req_ids, int n, float* mass, int cap, hipStream_t st) {
+    for (int i0 = 0; i0 < n; i0 += 128) {
+        sled_some_ids ids{};
+        const int here = std::min(n - i0, 128);
+        for (int i = 0; i < here; i++) ids.id[i] = req_ids[i0 + i];
+        hipLaunchKernelGGL(mass_clear_kernel, dim3(here), dim3(256), 0, st, ids, p->tail_dev, mass, cap, m->s.n_layers * m->s.n_kv_heads);
+        SLED_LAUNCH_CHECK();
+    }
+    return SLED_OK;
+}
+
 int sled_launch_tree_commit(const sled_model* m, const sled_kvpool* p, const int32_t* meta, const int32_t* pages, int B, const int32_t* accept_len,
                             const int32_t* path, float* mass, int cap, hipStream_t st) {
     const sled_shape& s = m->s;
-    commit_args a{meta, pages, p->len_dev, accept_len, path, mass, cap, s.n_layers, s.n_kv_heads, s.head_dim, p->k_pool, p->v_pool, p->n_pages};
+    commit_args a{meta, pages, p->len_dev, accept_len, path, mass, p->tail_dev, cap, s.n_layers, s.n_kv_heads, s.head_dim, p->k_pool, p->v_pool, p->n_pages};
     const dim3 grid(s.n_layers, B);
     if (s.dtype == SLED_BF16) hipLaunchKernelGGL((tree_commit_kernel<128, false>), grid, dim3(256), 0, st, a);
     else if (s.head_dim == 64) hipLaunchKernelGGL((tree_commit_kernel<64, true>), grid, dim3(256), 0, st, a);

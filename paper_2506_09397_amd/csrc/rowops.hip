@@ -585,20 +585,19 @@ __global__ __launch_bounds__(256) void copy_act_row_kernel(const void* __restric
 }
 
 // committed lengths after an append (+ add[i]) or, with `accept`, a commit (+ accept[i] + 1); `fresh`: the request starts from zero whatever the slot held
-__global__ void len_add_kernel(int32_t* __restrict__ len_dev, int32_t* __restrict__ shift_dev, const int32_t* __restrict__ req_ids,
-                               const int32_t* __restrict__ add, const int32_t* __restrict__ fresh, const int32_t* __restrict__ accept, int B) {
+__global__ void len_add_kernel(int32_t* __restrict__ len_dev, int32_t* __restrict__ shift_dev, int32_t* __restrict__ tail_dev,
+                               const int32_t* __restrict__ req_ids, const int32_t* __restrict__ add, const int32_t* __restrict__ fresh, const int32_t* __restrict__ accept, int B) {
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
     if (i >= B) return;
     const int r = req_ids[i], from = fresh && fresh[i] ? 0 : len_dev[r];
-    if (fresh && fresh[i]) shift_dev[r] = 0;
+    if (fresh && fresh[i]) shift_dev[r] = tail_dev[2 * r] = tail_dev[2 * r + 1] = 0;
     len_dev[r] = from + (accept ? accept[i] + 1 : add[i]);
 }
 // the lengths (and positions) of requests that have just been opened, up to 128 in a launch
-struct len_ids {
-    int id[128];
-};
-__global__ void len_zero_kernel(int32_t* __restrict__ len_dev, int32_t* __restrict__ shift_dev, len_ids ids, int n) {
-    if ((int)threadIdx.x < n) len_dev[ids.id[threadIdx.x]] = shift_dev[ids.id[threadIdx.x]] = 0;
+__global__ void len_zero_kernel(int32_t* __restrict__ len_dev, int32_t* __restrict__ shift_dev, int32_t* __restrict__ tail_dev, sled_some_ids ids, int n) {
+    if ((int)threadIdx.x >= n) return;
+    const int r = ids.id[threadIdx.x];
+    len_dev[r] = shift_dev[r] = tail_dev[2 * r] = tail_dev[2 * r + 1] = 0;
 }
 
 // ----- weight repacking --------------------------------------------------------------------
@@ -852,19 +851,19 @@ int sled_launch_kv_export(const sled_model* m, const sled_kvpool* p, void* k_dst
     return launch_kv_move<false>(m, p, &pc, 1, st);
 }
 
-int sled_launch_len_add(int32_t* len_dev, int32_t* shift_dev, const int32_t* req_ids_dev, const int32_t* add_dev, const int32_t* fresh_dev, const int32_t* accept_dev,
-                        int B, hipStream_t st) {
-    hipLaunchKernelGGL(len_add_kernel, dim3((B + 63) / 64), dim3(64), 0, st, len_dev, shift_dev, req_ids_dev, add_dev, fresh_dev, accept_dev, B);
+int sled_launch_len_add(const sled_kvpool* p, const int32_t* req_ids_dev, const int32_t* add_dev, const int32_t* fresh_dev, const int32_t* accept_dev, int B,
+                        hipStream_t st) {
+    hipLaunchKernelGGL(len_add_kernel, dim3((B + 63) / 64), dim3(64), 0, st, p->len_dev, p->shift_dev, p->tail_dev, req_ids_dev, add_dev, fresh_dev, accept_dev, B);
     SLED_LAUNCH_CHECK();
     return SLED_OK;
 }
 
-int sled_launch_len_zero(int32_t* len_dev, int32_t* shift_dev, const int* req_ids /*host*/, int n, hipStream_t st) {
+int sled_launch_len_zero(const sled_kvpool* p, const int* req_ids /*host*/, int n, hipStream_t st) {
     for (int i0 = 0; i0 < n; i0 += 128) {
-        len_ids ids{};
+        sled_some_ids ids{};
         const int here = std::min(n - i0, 128);
         for (int i = 0; i < here; i++) ids.id[i] = req_ids[i0 + i];
-        hipLaunchKernelGGL(len_zero_kernel, dim3(1), dim3(128), 0, st, len_dev, shift_dev, ids, here);
+        hipLaunchKernelGGL(len_zero_kernel, dim3(1), dim3(128), 0, st, p->len_dev, p->shift_dev, p->tail_dev, ids, here);
         SLED_LAUNCH_CHECK();
     }
     return SLED_OK;

@@ -168,6 +168,8 @@ struct sled_request {
     bool fresh = false;        // opened and not used yet: its device-side length is reset by the first call that has a stream
     int len_ub = 0;            // host-side upper bound of the committed length
     int staged = -1;           // k+1 of the last verify (rows staged), -1 if none
+    bool mass_added = false;   // the staged tree's nodes have mass in their slots (sled_tree_mass)
+    bool mass_left = false;    // a tree's nodes that were dropped since have: cleared by the next call that is given mass (tail_dev says where)
     int64_t added = 0;         // everything ever added to len_ub (lets a late read-back of the exact length be applied)
     uint32_t gen = 0;          // incarnation of the slot: a read-back taken for an earlier one is dropped
     std::vector<int> pages;
@@ -201,6 +203,7 @@ struct sled_kvpool {
     void* v_pool;
     int32_t* len_dev;          // [max_requests] committed context length of each request
     int32_t* shift_dev;        // [max_requests] tokens evicted so far: how far positions run ahead of the length
+    int32_t* tail_dev;         // [max_requests][2] slots in which nodes have mass, from and to (empty: none)
     std::vector<sled_request> reqs;
     std::vector<int> free_pages;
     std::vector<int> last_batch;   // request ids of the last verify
@@ -300,9 +303,9 @@ int sled_launch_kv_ingest(const sled_model* m, const sled_kvpool* p, const sled_
 int sled_launch_kv_export(const sled_model* m, const sled_kvpool* p, void* k_dst, void* v_dst, int first, int n_tokens,
                           const int32_t* pages_dev, hipStream_t st);
 // fresh_dev (or nullptr): nonzero where a request starts from length zero
-int sled_launch_len_add(int32_t* len_dev, int32_t* shift_dev, const int32_t* req_ids_dev, const int32_t* add_dev, const int32_t* fresh_dev, const int32_t* accept_dev,
-                        int B, hipStream_t st);
-int sled_launch_len_zero(int32_t* len_dev, int32_t* shift_dev, const int* req_ids /*host*/, int n, hipStream_t st);
+int sled_launch_len_add(const sled_kvpool* p, const int32_t* req_ids_dev, const int32_t* add_dev, const int32_t* fresh_dev, const int32_t* accept_dev, int B,
+                        hipStream_t st);
+int sled_launch_len_zero(const sled_kvpool* p, const int* req_ids /*host*/, int n, hipStream_t st);
 
 // tree.hip
 int sled_launch_tree_attention(const sled_model* m, const sled_kvpool* p, const sled_tree_plan& t, int layer, const void* q, size_t q_stride, size_t q_plane,
@@ -316,8 +319,14 @@ int sled_launch_tree_qkv(const sled_model* m, int T, const float* partial, int n
 constexpr int SLED_EVICT_REC = 5;
 int sled_launch_evict(const sled_model* m, const sled_kvpool* p, const int32_t* meta, const int32_t* pages, int B, int keep_max, int first, int recent, float* mass,
                       int cap, int32_t* idx, int idx_cap, bool in_place, hipStream_t st);
+int sled_launch_mass_clear(const sled_model* m, const sled_kvpool* p, const int* req_ids /*host*/, int n, float* mass, int cap, hipStream_t st);
 int sled_launch_tree_commit(const sled_model* m, const sled_kvpool* p, const int32_t* meta, const int32_t* pages, int B, const int32_t* accept_len,
                             const int32_t* path, float* mass, int cap, hipStream_t st);
+
+// ids of a launch that takes them by value
+struct sled_some_ids {
+    int id[128];
+};
 
 // accept_tree.hip
 size_t sled_accept_tree_ws_bytes(int B, int T, int vocab);

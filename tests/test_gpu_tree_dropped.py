@@ -1,0 +1,245 @@
+"""Trees whose nodes have got mass and are then dropped: nothing of it reaches the tokens that come to lie in their slots, or an eviction."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_09397_amd import sled, synth
+from gpu_common import build_verifier
+from tree_common import generator, plain_attention, pool, random_tree
+
+pytestmark = pytest.mark.gpu
+
+LAYERS, CAP = 2, 400
+
+
+class Steps:
+    """Requests of a pool, and steps over random trees on them that add up mass."""
+
+    def __init__(self, p, ctx, seed):
+        self.p, self.s, self.g, self.rng = p, p.shape, generator(seed), np.random.default_rng(seed)
+        opened = [p.open(L, self.g) for L in ctx]
+        self.reqs, self.K, self.V = [o[0] for o in opened], [o[1] for o in opened], [o[2] for o in opened]
+        self.mass = torch.zeros(16, LAYERS, self.s.n_kv_heads, CAP, device="cuda")
+        self.ws = p.workspace(len(ctx), 64 * len(ctx), sum(ctx) + 400)
+
+    def rows(self, n, h):
+        return torch.randn(LAYERS, n, h, self.s.head_dim, generator=self.g, device="cuda").to(self.p.dt)
+
+    def begin(self, nodes):
+        self.nodes, self.trees = nodes, [random_tree(self.rng, n) for n in nodes]
+        T = sum(nodes)
+        self.q, self.k, self.v = self.rows(T, self.s.n_q_heads), self.rows(T, self.s.n_kv_heads), self.rows(T, self.s.n_kv_heads)
+        sled.sled_tree_begin(self.p.pool, self.reqs, nodes, self.trees, self.ws)
+
+    def layers(self, with_mass=True):
+        self.lse = torch.empty(LAYERS, sum(self.nodes), self.s.n_q_heads, device="cuda")
+        for l in range(LAYERS):
+            sled.sled_tree_attention(self.p.pool, l, self.q[l], self.k[l], self.v[l], torch.empty_like(self.q[l]), self.lse[l], self.ws)
+            if with_mass:
+                sled.sled_tree_mass(self.p.pool, l, self.q[l], self.lse[l], self.mass, self.ws)
+
+    def step(self, nodes, with_mass=True):
+        self.begin(nodes)
+        self.layers(with_mass)
+
+    def exact(self, i):
+        """Mass that this step gives request i's tokens and nodes [layers, kv heads, L + n], in 64 bits."""
+        a = sum(self.nodes[:i])
+        at, n = slice(a, a + self.nodes[i]), self.nodes[i]
+        out = []
+        for l in range(LAYERS):
+            _, _, w, _, _ = plain_attention(self.q[l, at], self.K[i][l], self.V[i][l], self.k[l, at], self.v[l, at], self.trees[i])
+            out.append(w.reshape(n, self.s.n_kv_heads, self.s.group, -1).sum(dim=(0, 2)))
+        return torch.stack(out)
+
+    def append(self, i, n):
+        k, v = self.rows(n, self.s.n_kv_heads), self.rows(n, self.s.n_kv_heads)
+        sled.sled_kv_append(self.p.pool, [self.reqs[i]], [n], [k], [v])
+        self.K[i], self.V[i] = torch.cat([self.K[i], k], dim=1), torch.cat([self.V[i], v], dim=1)
+
+    def commit(self, paths, mass=True):
+        path, length = torch.full((len(paths), sled.TREE_MAX), -1, dtype=torch.int32), [len(w) for w in paths]
+        for i, w in enumerate(paths):
+            path[i, :len(w)] = torch.tensor(w, dtype=torch.int32)
+        sled.sled_tree_commit(self.p.pool, self.reqs, torch.tensor(length, dtype=torch.int32, device="cuda"), path.cuda(), self.mass if mass else None)
+
+
+def close(got, want):
+    """A score is a float32 sum of 128 products whose magnitudes add up to 12 at most here, (128 + 8) 2^-24 of that, 1e-4; a weight is off by as much once
+    more through its row's lse, and a sum of up to 256 of them by 256 2^-24."""
+    assert bool(((got.double() - want).abs() <= 3e-4 * want).all())
+
+
+HEADS = {"8b": (32, 8, 128, "bf16"), "f32_64": (4, 4, 64, "f32")}
+
+
+@pytest.mark.parametrize("heads", list(HEADS))
+def test_a_smaller_tree_in_the_place_of_a_larger_one(heads):
+    with pool(*HEADS[heads], layers=LAYERS) as p:
+        t = Steps(p, [100, 0, 31], seed=1)
+        t.step([10, 64, 5])
+        first = [t.exact(i) for i in range(3)]
+        t.step([3, 1, 5])
+        second = [t.exact(i) for i in range(3)]
+        for i, (L, n) in enumerate(zip([100, 0, 31], t.nodes)):
+            got = t.mass[t.reqs[i]]
+            close(got[..., :L], first[i][..., :L] + second[i][..., :L])
+            close(got[..., L:L + n], second[i][..., L:])
+            assert bool((got[..., L + n:] == 0).all())
+        t.commit([[], [], []])
+        for i, L in enumerate([100, 0, 31]):
+            close(t.mass[t.reqs[i], :, :, L], second[i][..., L])
+            assert bool((t.mass[t.reqs[i], :, :, L + 1:] == 0).all())
+
+
+@pytest.mark.parametrize("dropped_by", ["append", "a tree without mass", "its own commit without mass"])
+def test_tokens_in_a_dropped_nodes_slot_start_from_zero(dropped_by):
+    with pool(*HEADS["8b"], layers=LAYERS) as p:
+        t = Steps(p, [60], seed=2)
+        t.step([20])
+        first = t.exact(0)
+        if dropped_by == "append":
+            t.append(0, 7)
+        elif dropped_by == "a tree without mass":
+            t.step([4], with_mass=False)
+            t.K[0], t.V[0] = torch.cat([t.K[0], t.k[:, :1]], dim=1), torch.cat([t.V[0], t.v[:, :1]], dim=1)
+            t.commit([[]], mass=False)
+        else:
+            t.K[0], t.V[0] = torch.cat([t.K[0], t.k[:, :1]], dim=1), torch.cat([t.V[0], t.v[:, :1]], dim=1)
+            t.commit([[]], mass=False)
+        t.step([2])
+        second, L = t.exact(0), t.K[0].shape[1]
+        got = t.mass[t.reqs[0]]
+        close(got[..., :60], first[..., :60] + second[..., :60])
+        close(got[..., 60:L + 2], second[..., 60:])
+        assert bool((got[..., L + 2:] == 0).all())
+
+
+def test_a_commit_does_not_move_the_mass_of_other_nodes():
+    """The second tree gets no mass itself: what its nodes' slots hold is the first one's."""
+    with pool(*HEADS["8b"], layers=LAYERS) as p:
+        t = Steps(p, [50], seed=3)
+        t.step([30])
+        first = t.exact(0)
+        t.step([12], with_mass=False)
+        t.commit([[]])
+        close(t.mass[t.reqs[0], :, :, :50], first[..., :50])
+        assert bool((t.mass[t.reqs[0], :, :, 50:] == 0).all())
+
+
+@pytest.mark.parametrize("keep", [30, 80, 300])
+def test_evictions_leave_nothing_of_a_staged_tree(keep):
+    with pool(*HEADS["8b"], layers=LAYERS) as p:
+        t = Steps(p, [80, 90], seed=4)
+        t.step([25, 40])
+        ws = sled.workspace(sled.sled_kv_evict_workspace_bytes(p.model, 2, 300))
+        sled.sled_kv_evict(p.pool, t.reqs, [keep, keep], 2, 4, t.mass, ws)
+        for r, L in zip(t.reqs, (80, 90)):
+            n = min(keep, L)
+            assert bool((t.mass[r, :, :, n:] == 0).all()) and bool((t.mass[r, :, :, :n] > 0).all())
+
+
+def test_an_eviction_into_another_request_keeps_the_staged_tree_and_its_mass():
+    with pool(*HEADS["8b"], layers=LAYERS) as p:
+        t = Steps(p, [80], seed=5)
+        t.step([25])
+        exact = t.exact(0)
+        dst = sled.sled_kvpool_open(p.pool)
+        # the destination once had a tree of its own, dropped while it was empty
+        own = t.reqs
+        t.reqs, K, V = [dst], t.K, t.V
+        t.K, t.V = [t.K[0][:, :0]], [t.V[0][:, :0]]
+        q = t.q, t.k, t.v, t.nodes, t.trees
+        t.step([9])
+        t.append(0, 0)
+        t.reqs, t.K, t.V = own, K, V
+        t.q, t.k, t.v, t.nodes, t.trees = q
+        t.step([25])                          # (the plan at hand is the pool's last one: once more)
+        again = t.exact(0)
+        ws = sled.workspace(sled.sled_kv_evict_workspace_bytes(p.model, 1, 30))
+        sled.sled_kv_evict(p.pool, t.reqs, [30], 2, 4, t.mass, ws, dst_ids=[dst])
+        kept = t.mass[dst, :, :, :30].clone()
+        assert bool((kept > 0).all()) and bool((t.mass[dst, :, :, 30:] == 0).all())
+        close(t.mass[t.reqs[0], :, :, :105], torch.cat([exact[..., :80] + again[..., :80], again[..., 80:]], dim=2))
+        t.commit([[]])
+        close(t.mass[t.reqs[0], :, :, 80], again[..., 80])
+        k2, v2 = p.read(dst, 0, 30)
+        t.reqs, t.K, t.V = [dst], [k2], [v2]
+        t.step([3])
+        close(t.mass[dst, :, :, :33], torch.cat([kept.double(), torch.zeros_like(kept[..., :3]).double()], dim=2) + t.exact(0))
+
+
+def test_a_slot_used_again_starts_afresh():
+    with pool(*HEADS["8b"], layers=LAYERS, max_requests=1) as p:
+        t = Steps(p, [40], seed=6)
+        t.mass = t.mass[:1].contiguous()
+        t.step([30])
+        sled.sled_kvpool_close(p.pool, t.reqs[0])
+        r, t.K[0], t.V[0] = p.open(65, t.g)
+        assert r == t.reqs[0]
+        t.mass.zero_()
+        t.mass[0, :, :, :65] = 0.5            # the mass that came with the context
+        t.step([2])
+        close(t.mass[0, :, :, :65], 0.5 + t.exact(0)[..., :65])
+
+
+def test_a_captured_call_does_not_clear():
+    with pool(*HEADS["8b"], layers=LAYERS) as p:
+        t = Steps(p, [40], seed=7)
+        t.step([30])
+        first = t.exact(0)
+        t.begin([3])
+        t.layers(with_mass=False)
+        torch.cuda.synchronize()
+        error, x = None, torch.zeros(4, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            x += 1
+            try:
+                sled.sled_tree_mass(p.pool, 0, t.q[0], t.lse[0], t.mass, t.ws)
+            except sled.SledError as e:
+                error = e
+        assert error is not None and error.code == sled.ESTATE and "captured" in str(error)
+        before = t.mass.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(t.mass, before)
+        sled.sled_tree_mass(p.pool, 0, t.q[0], t.lse[0], t.mass, t.ws)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            sled.sled_tree_mass(p.pool, 1, t.q[1], t.lse[1], t.mass, t.ws)
+        graph.replay()
+        torch.cuda.synchronize()
+        second = t.exact(0)
+        close(t.mass[t.reqs[0], :, :, :43], torch.cat([first[..., :40] + second[..., :40], second[..., 40:]], dim=2))
+        assert bool((t.mass[t.reqs[0], :, :, 43:] == 0).all())
+
+
+@pytest.mark.parametrize("dropped_by", ["prefill", "chain"])
+def test_prompts_and_chains_in_a_dropped_trees_place(dropped_by):
+    """Two requests with the same tokens and caches, one of which had a tree with mass in between: the next step gives both the same mass."""
+    shape = synth.SHAPES["tiny"]
+    v, w = build_verifier(shape, 3, n_pages=60, max_requests=2, B_max=2, ctx_tokens_max=400, gain_jitter=0.1, std=0.08)
+    v.enable_trees(20, 200, mass_cap=160, max_requests=2)
+    rng = np.random.default_rng(5)
+    ids = lambda n: torch.from_numpy(rng.integers(0, shape.vocab, size=n).astype(np.int32)).cuda()
+    prompt, more, tree, tok = ids(45), ids(6), random_tree(rng, 20), ids(20)
+    a, b = v.open_bounded(), v.open_bounded()
+    for r in (a, b):
+        v.prefill(r, prompt, want_logits=False)
+    v.verify_tree([a], [tree], tok)
+    first = v.mass[a, :, :, :45].clone()
+    if dropped_by == "prefill":
+        for r in (a, b):
+            v.prefill(r, more, want_logits=False)
+    else:
+        v.verify([a, b], [5, 5], torch.cat([more, more]))
+        v.commit([a, b], torch.full((2,), 5, dtype=torch.int32, device="cuda"))
+    assert v.lengths([a, b]) == [51, 51]
+    v.verify_tree([a, b], [[-1, 0, 0], [-1, 0, 0]], torch.cat([tok[:3], tok[:3]]))
+    got = v.mass[a].clone()
+    got[..., :45] -= first
+    # (the caches of a and b may differ in their last bits: they were made in other batches)
+    assert float((got - v.mass[b]).abs().max()) < 1e-4
+    assert bool((got[..., 54:] == 0).all())
+    v.destroy()
