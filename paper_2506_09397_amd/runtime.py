@@ -84,7 +84,8 @@ class Verifier:
         """Buffers for steps over trees of up to nodes_max nodes on contexts of ctx_tokens_max tokens together.  mass_cap > 0: the weight that
         attention gives the tokens of up to max_requests requests of up to mass_cap tokens (nodes included) is added up, for evict()."""
         s, B = self.shape, self.B_max
-        T = B * nodes_max
+        self.nodes_max = min(nodes_max, sled.TREE_MAX)
+        T = B * self.nodes_max
         self.tree_ws = sled.workspace(sled.sled_verify_tree_workspace_bytes(self.model, B, T, ctx_tokens_max + T))
         self.tree_acc_ws = sled.workspace(sled.sled_accept_tree_workspace_bytes(B, T, s.vocab))
         self.tree_logits = torch.empty(T, s.vocab, dtype=torch.float32, device="cuda")

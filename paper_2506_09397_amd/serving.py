@@ -149,7 +149,8 @@ class Server:
                 raise ValueError(f"device {device}: round {round_no} is older than the last answered round {last.round_no}")
             return dataclasses.replace(last, replayed=True)
         if self.trees:
-            drafts = [int(d) for d in drafts][: sled.TREE_MAX - 1]
+            # (like a chain's: what the verifier's buffers do not hold is drafted again; a node comes behind the one it continues, so a front part is a tree)
+            drafts = [int(d) for d in drafts][: min(sled.TREE_MAX, getattr(self.v, "nodes_max", sled.TREE_MAX)) - 1]
             up = list(range(len(drafts))) if parents is None else [int(x) for x in parents][: len(drafts)]
             if len(up) != len(drafts) or any(not 0 <= x <= j for j, x in enumerate(up)):
                 raise ValueError(f"device {device}: every draft continues a node that comes before it")

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import test_gpu_accept_tree as accept
-from paper_2506_09397_amd import sled, synth
+from paper_2506_09397_amd import serving, sled, synth
 from paper_2506_09397_amd.runtime import Verifier
 from tree_common import random_tree
 
@@ -40,4 +40,21 @@ def test_a_verifier_for_many_large_trees_accepts_small_batches():
         v.commit_tree(reqs[:B], a, path)
         want, _ = accept.walk(sled.GREEDY, trees, logits.cpu().numpy(), tokens.cpu().numpy(), None, 1.0)
         assert [(int(x), p, int(y)) for x, p, y in zip(a.tolist(), path.tolist(), t.tolist())] == want
+    v.destroy()
+
+
+def test_a_device_that_drafts_more_than_the_verifier_holds():
+    """Its tree is cut; the other devices of the batch get their answers."""
+    shape = synth.SHAPES["tiny_bf16"]
+    v = Verifier(shape, synth.SynthWeights(shape, seed=1, device="cuda"), 60, 3, 3, 400)
+    v.enable_trees(6, 200, mass_cap=60, max_requests=3)
+    server = serving.Server(v, 3, trees=True, kv_budget=48, kv_recent=8)
+    for d in range(3):
+        server.open(d, prompt=list(range(10 + d)))
+    server.submit(0, 0, 7, [1, 2, 3])
+    server.submit(1, 0, 7, list(range(63)), parents=[0] * 63)
+    server.submit(2, 0, 7, [5])
+    answers = server.run_batch()
+    assert [r.device for r in answers] == [0, 1, 2]
+    assert v.lengths([server.req_of[d] for d in range(3)]) == [10 + d + r.accept_len + 1 for d, r in enumerate(answers)]
     v.destroy()
