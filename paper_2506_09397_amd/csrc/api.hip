@@ -843,8 +843,9 @@ struct step_entry {
 // (nothing is committed here), and the logits of all rows go to logits_all [T, vocab], or those of the single row
 // one_row to logits_one [vocab], or nowhere.
 // tr: the blocks are trees, attended to by the plan that sled_tree_begin's part of the work has made.
+// started: set once something is launched, from when on the requests' tail slots may have been written even if the call fails.
 int run_forward(sled_model* m, sled_kvpool* p, const std::vector<step_entry>& ent, const int32_t* tokens, float* logits_all,
-                int one_row, float* logits_one, void* workspace, size_t workspace_bytes, hipStream_t st, const char* who, const tree_step* tr = nullptr) {
+                int one_row, float* logits_one, void* workspace, size_t workspace_bytes, hipStream_t st, const char* who, const tree_step* tr = nullptr, bool* started = nullptr) {
     const sled_shape& s = m->s;
     const int B = (int)ent.size();
     const int Hkv = s.n_kv_heads, G = s.n_q_heads / Hkv;
@@ -1000,6 +1001,7 @@ int run_forward(sled_model* m, sled_kvpool* p, const std::vector<step_entry>& en
         SLED_TRY(x);                       \
     } while (0)
 
+    if (started) *started = true;
     SLED_RUN(SLED_PROF_ROWS, sled_launch_step_setup(m, p, meta, tokens, cs, kvslot, plan, arrive, h, xa, pl_d, m->layers[0].g_attn, st));
     for (int l = 0; l < s.n_layers; l++) {
         const sled_layer_weights& w = m->layers[l];
@@ -1058,9 +1060,16 @@ extern "C" int sled_verify_batch(sled_model* m, sled_kvpool* p, int B, const int
     }
     poll_readbacks(p);
     if ((rc = reset_fresh_lengths(p, B, req_ids, static_cast<hipStream_t>(stream))) != SLED_OK) return rc;
+    bool started = false;
     rc = run_forward(m, p, ent, tokens, logits, -1, nullptr, workspace, workspace_bytes, static_cast<hipStream_t>(stream),
-                     "sled_verify_batch");
-    if (rc != SLED_OK) return rc;
+                     "sled_verify_batch", nullptr, &started);
+    if (rc != SLED_OK) {
+        for (int i = 0; started && i < B; i++) {   // what was staged there before is half overwritten
+            leave_tree(p, req_ids[i]);
+            p->reqs[req_ids[i]].staged = -1;
+        }
+        return rc;
+    }
     // what an earlier verify staged for requests that are not in this batch stays staged, but only the last batch
     // can be committed
     for (int r : p->last_batch) p->reqs[r].staged = -1;
@@ -1473,6 +1482,7 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
                 memcpy(mass_item, rec, sizeof(rec));
             }
     }
+    p->tree.valid = false;   // (what the workspace held, if it is the same one)
     SLED_HIP(hipMemcpyAsync(workspace, sl->host, w.ints, hipMemcpyHostToDevice, st));
     if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
     char* ws = static_cast<char*>(workspace);
@@ -1680,7 +1690,8 @@ extern "C" int sled_verify_tree(sled_model* m, sled_kvpool* p, int B, const int*
     if (w.plan > workspace_bytes) SLED_FAIL(SLED_EINVAL, "sled_verify_tree: workspace of %zu bytes, more than %zu needed", workspace_bytes, w.plan);
     char* ws = static_cast<char*>(workspace);
     if ((rc = plan_trees(p, B, req_ids, n_nodes, parent, ws + w.plan, workspace_bytes - w.plan, st, "sled_verify_tree")) != SLED_OK) return rc;
-    p->tree.valid = false;   // (the plan serves this step alone; the nodes stay staged for the commit)
+    p->tree.valid = false;   // (the plan serves this step alone)
+    for (int i = 0; i < B; i++) p->reqs[req_ids[i]].staged = -1;   // nothing to commit until all of it is on its way
     if (mass) {
         if ((rc = clear_mass(p, B, req_ids, false, mass, mass_cap, st, "sled_verify_tree")) != SLED_OK) return rc;
         for (int i = 0; i < B; i++) p->reqs[req_ids[i]].mass_added = true;
@@ -1688,7 +1699,9 @@ extern "C" int sled_verify_tree(sled_model* m, sled_kvpool* p, int B, const int*
     std::vector<step_entry> ent(B);
     for (int i = 0; i < B; i++) ent[i] = step_entry{req_ids[i], 0, n_nodes[i]};
     const tree_step tr{&p->tree.plan, depth.data(), ws + w.k, ws + w.v, reinterpret_cast<float*>(ws + w.lse), mass, mass_cap};
-    return run_forward(m, p, ent, tokens, logits, -1, nullptr, workspace, w.k, st, "sled_verify_tree", &tr);
+    if ((rc = run_forward(m, p, ent, tokens, logits, -1, nullptr, workspace, w.k, st, "sled_verify_tree", &tr)) != SLED_OK) return rc;
+    for (int i = 0; i < B; i++) p->reqs[req_ids[i]].staged = n_nodes[i];
+    return SLED_OK;
 }
 SLED_CATCH("sled_verify_tree")
 
