@@ -630,6 +630,10 @@ extern "C" int sled_kv_append(sled_kvpool* p, int B, const int* req_ids, const i
         for (int pg : rq.pages) sl->host[off++] = pg;
     }
     SLED_HIP(hipMemcpyAsync(sl->dev, sl->host, off * sizeof(int32_t), hipMemcpyHostToDevice, st));
+    for (int i = 0; i < B; i++) {
+        leave_tree(p, req_ids[i]);
+        p->reqs[req_ids[i]].staged = -1;   // rows staged by an uncommitted step are overwritten: nothing of this request is left to commit
+    }
     if ((rc = sled_launch_kv_ingest(m, p, pieces.data(), (int)pieces.size(), st)) != SLED_OK) return rc;
     if ((rc = sled_launch_len_add(p, sl->dev, sl->dev + B, sl->dev + 2 * B, nullptr, B, st)) != SLED_OK) return rc;
     if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
@@ -638,8 +642,6 @@ extern "C" int sled_kv_append(sled_kvpool* p, int B, const int* req_ids, const i
         rq.fresh = false;
         rq.len_ub += n_tokens[i];
         rq.added += n_tokens[i];
-        leave_tree(p, req_ids[i]);
-        rq.staged = -1;   // rows staged by an uncommitted verify are overwritten: nothing of this request is left to commit
     }
     return SLED_OK;
 }
@@ -1654,16 +1656,16 @@ extern "C" int sled_tree_commit(sled_kvpool* p, int B, const int* req_ids, const
         for (int pg : rq.pages) sl->host[off++] = pg;
     }
     SLED_HIP(hipMemcpyAsync(sl->dev, sl->host, off * sizeof(int32_t), hipMemcpyHostToDevice, st));
-    if ((rc = sled_launch_tree_commit(p->m, p, sl->dev, sl->dev + 3 * B, B, accept_len, path, mass, mass_cap, st)) != SLED_OK) return rc;
-    if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
-    for (int i = 0; i < B; i++) {
+    for (int i = 0; i < B; i++) {   // (before the launches: should one of them fail, the nodes may have moved and cannot be committed again)
         sled_request& rq = p->reqs[req_ids[i]];
         rq.len_ub += rq.staged;   // every node of a chain may have been accepted; the exact lengths follow
         rq.added += rq.staged;
         rq.staged = -1;
-        if (mass) rq.mass_added = false;
         leave_tree(p, req_ids[i]);
     }
+    if ((rc = sled_launch_tree_commit(p->m, p, sl->dev, sl->dev + 3 * B, B, accept_len, path, mass, mass_cap, st)) != SLED_OK) return rc;
+    for (int i = 0; mass && i < B; i++) p->reqs[req_ids[i]].mass_left = false;   // moved with its nodes, or cleared
+    if ((rc = stage_release(sl, st)) != SLED_OK) return rc;
     return enqueue_readback(p, B, req_ids, st);
 }
 SLED_CATCH("sled_tree_commit")

@@ -85,6 +85,24 @@ def test_a_chain_step_that_fails_drops_what_its_requests_had_staged(kind):
     v.destroy()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_commit_or_an_append_that_fails_drops_what_was_staged(kind):
+    t = Rounds(kind)
+    v, s = t.v, t.shape
+    K, V = (torch.randn(s.n_layers, 2, s.n_kv_heads, s.head_dim, device="cuda").to(s.torch_dtype) for _ in range(2))
+    v.verify_tree(t.reqs, t.trees, t.tokens)
+    t.fails(lambda: v.append_context(t.reqs[:1], [K], [V]))
+    t.no_commit(lambda: v.commit_tree(t.reqs[:1], t.none[:1], t.path[:1]))
+    t.fails(lambda: v.commit_tree(t.reqs[1:2], t.none[1:2], t.path[1:2]))
+    t.no_commit(lambda: v.commit_tree(t.reqs[1:2], t.none[:1], t.path[:1]))
+    v.commit_tree(t.reqs[2:], t.none[:1], t.path[:1])
+    assert v.lengths(t.reqs) == [20, 33, 8]
+    v.verify_tree(t.reqs, t.trees, t.tokens)
+    v.commit_tree(t.reqs, t.none, t.path)
+    assert v.lengths(t.reqs) == [21, 34, 9]
+    v.destroy()
+
+
 def test_a_refused_step_leaves_what_is_staged():
     """Nothing is launched by a call whose arguments are refused."""
     t = Rounds("tiny_bf16")
