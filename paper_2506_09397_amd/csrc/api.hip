@@ -1499,7 +1499,6 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
     t.n_items = (int)n_items;
     t.n_mass_items = (int)n_mass;
     t.max_nodes = nmax;
-    t.T = T;
     // what earlier steps staged for these requests is overwritten, and only the last trees can be committed
     for (int r : p->tree.reqs) {
         p->reqs[r].staged = -1;

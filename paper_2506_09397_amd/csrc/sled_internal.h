@@ -191,7 +191,7 @@ struct sled_tree_plan {
     float* part_o;               // states of split items
     float* part_ml;
     int n_items, n_mass_items;
-    int max_nodes, T;
+    int max_nodes;
 };
 
 struct sled_kvpool {

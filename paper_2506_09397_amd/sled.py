@@ -12,7 +12,7 @@ import ctypes as C
 import itertools
 import os
 import struct
-from typing import Optional, Sequence
+from typing import Dict, Optional, Sequence
 
 import torch
 
@@ -143,6 +143,24 @@ def _stream() -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+class _PoolInfo:
+    """What a pool's tensors have to look like; the C entry points see pointers alone."""
+
+    def __init__(self, shape: ModelShape, max_requests: int):
+        self.dtype = shape.torch_dtype
+        self.q_row, self.kv_row = (shape.n_q_heads, shape.head_dim), (shape.n_kv_heads, shape.head_dim)
+        self.mass = (max_requests, shape.n_layers, shape.n_kv_heads)
+        self.plan(0)
+
+    def plan(self, rows: int) -> None:
+        """The trees that sled_tree_begin has planned last have so many nodes (0: none so far, the library refuses what comes)."""
+        self.rows, self.q, self.kv, self.lse = rows, (rows, *self.q_row), (rows, *self.kv_row), (rows, self.q_row[0])
+
+
+_models: Dict[int, ModelShape] = {}
+_pools: Dict[int, _PoolInfo] = {}
+
+
 # ---------------------------------------------------------------------------------------- model
 def sled_model_create(shape: ModelShape) -> int:
     s = _Shape(shape.n_layers, shape.d_model, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.d_ffn,
@@ -150,6 +168,7 @@ def sled_model_create(shape: ModelShape) -> int:
                shape.k_max)
     h = C.c_void_p()
     _check(lib().sled_model_create(C.byref(s), C.byref(h)))
+    _models[h.value] = shape
     return h.value
 
 
@@ -158,6 +177,7 @@ def sled_model_load(model: int, tensor_id: int, layer: int, src: torch.Tensor) -
 
 
 def sled_model_destroy(model: int) -> None:
+    _models.pop(model, None)
     _check(lib().sled_model_destroy(model))
 
 
@@ -165,6 +185,7 @@ def sled_model_destroy(model: int) -> None:
 def sled_kvpool_create(model: int, n_pages: int, max_requests: int) -> int:
     h = C.c_void_p()
     _check(lib().sled_kvpool_create(model, n_pages, max_requests, C.byref(h)))
+    _pools[h.value] = _PoolInfo(_models[model], max_requests)
     return h.value
 
 
@@ -185,6 +206,7 @@ def sled_kvpool_lengths(pool: int, req_ids: Sequence[int]):
 
 
 def sled_kvpool_destroy(pool: int) -> None:
+    _pools.pop(pool, None)
     _check(lib().sled_kvpool_destroy(pool))
 
 
@@ -336,11 +358,13 @@ def _bytes(t: torch.Tensor) -> int:
     return t.numel() * t.element_size()
 
 
-def _mass(mass: Optional[torch.Tensor]):
+def _mass(pool: int, mass: Optional[torch.Tensor]):
     """(pointer, entries of a row) of a [max_requests, n_layers, n_kv_heads, cap] float32 tensor."""
     if mass is None:
         return None, 0
-    assert mass.dtype == torch.float32 and mass.dim() == 4
+    assert mass.dtype == torch.float32 and mass.dim() == 4, "mass: float32 [max_requests, n_layers, n_kv_heads, entries]"
+    info = _pools.get(pool)
+    assert info is None or (mass.shape[0] >= info.mass[0] and mass.shape[1:3] == info.mass[1:]), f"mass {tuple(mass.shape)}: the pool has {info.mass}"
     return _ptr(mass), int(mass.shape[3])
 
 
@@ -351,24 +375,31 @@ def sled_tree_workspace_bytes(model: int, B_max: int, T_max: int, ctx_tokens_max
 def sled_tree_begin(pool: int, req_ids: Sequence[int], n_nodes: Sequence[int], parents: Sequence[Sequence[int]], workspace: torch.Tensor) -> None:
     assert len(req_ids) == len(n_nodes)
     _check(lib().sled_tree_begin(pool, len(req_ids), _packed(req_ids), _packed(n_nodes), _parents(n_nodes, parents), _ptr(workspace), _bytes(workspace), _stream()))
+    if pool in _pools:
+        _pools[pool].plan(sum(n_nodes))
 
 
 def sled_tree_attention(pool: int, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor],
                         workspace: torch.Tensor) -> None:
-    rows, kv_rows, dtype = q.shape, k.shape, q.dtype
+    rows, kv_rows, dtype, info = q.shape, k.shape, q.dtype, _pools.get(pool)
+    assert info is None or not info.rows or (rows == info.q and kv_rows == info.kv and dtype is info.dtype), \
+        f"q {tuple(rows)}, k {tuple(kv_rows)} of {dtype}: the trees at hand take {info.q}, {info.kv} of {info.dtype}"
     assert k.dtype is dtype and v.dtype is dtype and out.dtype is dtype and (lse is None or lse.dtype is torch.float32)
     assert rows[0] == kv_rows[0] and v.shape == kv_rows and out.shape == rows and (lse is None or lse.shape == rows[:2])
     _check(lib().sled_tree_attention(pool, int(layer), *_rows(q, rows), *_rows(k, kv_rows), *_rows(v, kv_rows), _ptr(out), _ptr(lse), _ptr(workspace), _stream()))
 
 
 def sled_tree_mass(pool: int, layer: int, q: torch.Tensor, lse: torch.Tensor, mass: torch.Tensor, workspace: torch.Tensor) -> None:
+    info = _pools.get(pool)
     assert lse.dtype == torch.float32 and lse.shape == q.shape[:2]
-    _check(lib().sled_tree_mass(pool, int(layer), *_rows(q, q.shape), _ptr(lse), *_mass(mass), _ptr(workspace), _stream()))
+    assert info is None or not info.rows or (q.shape == info.q and q.dtype is info.dtype), \
+        f"q {tuple(q.shape)} of {q.dtype}: the trees at hand take {info.q} of {info.dtype}"
+    _check(lib().sled_tree_mass(pool, int(layer), *_rows(q, q.shape), _ptr(lse), *_mass(pool, mass), _ptr(workspace), _stream()))
 
 
 def sled_tree_commit(pool: int, req_ids: Sequence[int], accept_len: torch.Tensor, path: torch.Tensor, mass: Optional[torch.Tensor] = None) -> None:
     assert accept_len.dtype == torch.int32 and path.dtype == torch.int32 and tuple(path.shape) == (len(req_ids), TREE_MAX) and accept_len.numel() == len(req_ids)
-    _check(lib().sled_tree_commit(pool, len(req_ids), _packed(req_ids), _ptr(accept_len), _ptr(path), *_mass(mass), _stream()))
+    _check(lib().sled_tree_commit(pool, len(req_ids), _packed(req_ids), _ptr(accept_len), _ptr(path), *_mass(pool, mass), _stream()))
 
 
 def sled_verify_tree_workspace_bytes(model: int, B_max: int, T_max: int, ctx_tokens_max: int) -> int:
@@ -378,8 +409,9 @@ def sled_verify_tree_workspace_bytes(model: int, B_max: int, T_max: int, ctx_tok
 def sled_verify_tree(model: int, pool: int, req_ids: Sequence[int], n_nodes: Sequence[int], parents: Sequence[Sequence[int]], tokens: torch.Tensor,
                      logits: torch.Tensor, workspace: torch.Tensor, mass: Optional[torch.Tensor] = None) -> None:
     assert tokens.dtype == torch.int32 and logits.dtype == torch.float32 and len(req_ids) == len(n_nodes)
-    assert tokens.numel() == sum(n_nodes) and logits.shape[0] == sum(n_nodes)
-    _check(lib().sled_verify_tree(model, pool, len(req_ids), _packed(req_ids), _packed(n_nodes), _parents(n_nodes, parents), _ptr(tokens), _ptr(logits), *_mass(mass),
+    assert tokens.numel() == sum(n_nodes) and logits.dim() == 2 and logits.shape[0] == sum(n_nodes)
+    assert model not in _models or logits.shape[1] == _models[model].vocab, f"logits of {logits.shape[1]} values a row, the model has {_models[model].vocab}"
+    _check(lib().sled_verify_tree(model, pool, len(req_ids), _packed(req_ids), _packed(n_nodes), _parents(n_nodes, parents), _ptr(tokens), _ptr(logits), *_mass(pool, mass),
                                   _ptr(workspace), _bytes(workspace), _stream()))
 
 
@@ -407,7 +439,7 @@ def sled_kv_evict(pool: int, req_ids: Sequence[int], keep: Sequence[int], n_firs
                   dst_ids: Optional[Sequence[int]] = None) -> None:
     assert len(keep) == len(req_ids) and (dst_ids is None or len(dst_ids) == len(req_ids))
     _check(lib().sled_kv_evict(pool, len(req_ids), _packed(req_ids), None if dst_ids is None else _packed(dst_ids), _packed(keep), int(n_first), int(n_recent),
-                               *_mass(mass), _ptr(workspace), _bytes(workspace), _stream()))
+                               *_mass(pool, mass), _ptr(workspace), _bytes(workspace), _stream()))
 
 
 def sled_kvpool_positions(pool: int, req_ids: Sequence[int]):
