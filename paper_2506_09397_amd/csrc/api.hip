@@ -443,7 +443,7 @@ extern "C" int sled_kvpool_open(sled_kvpool* p, int* req_id) {
 // A request's staged tree goes without a commit that knows its mass: what its nodes have got stays behind.
 static void drop_mass(sled_request& rq) {
     rq.mass_left = rq.mass_left || rq.mass_added;
-    rq.mass_added = false;
+    rq.mass_added = rq.mass_noted = false;
 }
 
 // A request's length or pages change, or its tail slots are overwritten: the trees at hand cannot be attended to any more, and this request's
@@ -1534,23 +1534,42 @@ int check_mass(const sled_kvpool* p, int mass_cap, int reach, const char* who) {
     return SLED_OK;
 }
 
-// Before mass is read or added to: slots in which dropped nodes have left some are cleared.  staged: also those of the trees at hand, which go now.
-int clear_mass(sled_kvpool* p, int B, const int* req_ids, bool staged, float* mass, int mass_cap, hipStream_t st, const char* who) {
-    std::vector<int> ids;
+// Before mass is read or added to: slots in which dropped nodes have left some are cleared.  nodes: what these requests' trees have, which get mass now (once
+// a plan: a launch per layer would cost more than the note is worth).  going: so do the trees at hand, with what they have got.
+int open_mass(sled_kvpool* p, int B, const int* req_ids, const int* nodes, bool going, float* mass, int mass_cap, hipStream_t st, const char* who) {
+    bool some = false, left = false;
+    auto has_left = [&](const sled_request& rq) { return rq.mass_left || (going && rq.mass_added); };
     for (int i = 0; i < B; i++) {
         const sled_request& rq = p->reqs[req_ids[i]];
-        if (rq.mass_left || (staged && rq.mass_added)) ids.push_back(req_ids[i]);
+        left = left || has_left(rq);
+        some = some || has_left(rq) || (nodes && !rq.mass_noted);
     }
-    if (ids.empty()) return SLED_OK;
+    if (!some) return SLED_OK;
+    int rc;
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
     SLED_HIP(hipStreamIsCapturing(st, &status));
-    if (status != hipStreamCaptureStatusNone)
+    const bool captured = status != hipStreamCaptureStatusNone;
+    if (left && captured)
         SLED_FAIL(SLED_ESTATE, "%s: a dropped tree has left mass, which cannot be cleared by a captured call (make one first that is not captured)", who);
-    int rc;
-    if ((rc = sled_launch_mass_clear(p->m, p, ids.data(), (int)ids.size(), mass, mass_cap, st)) != SLED_OK) return rc;
-    for (int r : ids) {
-        p->reqs[r].mass_left = false;
-        if (staged) p->reqs[r].mass_added = false;
+    for (int i0 = 0; i0 < B; i0 += SLED_MASS_IDS) {
+        sled_mass_ids ids{};
+        int n = 0;
+        for (int i = i0; i < std::min(B, i0 + SLED_MASS_IDS); i++) {
+            const sled_request& rq = p->reqs[req_ids[i]];
+            if (!nodes && !has_left(rq)) continue;
+            ids.id[n] = req_ids[i];
+            ids.nodes[n] = nodes ? (uint8_t)nodes[i] : 0;
+            ids.left[n++] = has_left(rq);
+        }
+        if (n && (rc = sled_launch_mass_open(p->m, p, ids, n, mass, mass_cap, st)) != SLED_OK) return rc;
+    }
+    for (int i = 0; i < B; i++) {
+        sled_request& rq = p->reqs[req_ids[i]];
+        rq.mass_left = false;
+        if (going) rq.mass_added = rq.mass_noted = false;
+        if (!nodes) continue;
+        rq.mass_added = true;
+        rq.mass_noted = rq.mass_noted || !captured;
     }
     return SLED_OK;
 }
@@ -1622,8 +1641,11 @@ extern "C" int sled_tree_mass(sled_kvpool* p, int layer, const void* q, int64_t 
     if ((rc = check_rows(m, q, q_stride, m->s.n_q_heads * m->s.head_dim, "q", "sled_tree_mass")) != SLED_OK) return rc;
     if ((rc = check_mass(p, mass_cap, p->tree.max_reach, "sled_tree_mass")) != SLED_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if ((rc = clear_mass(p, (int)p->tree.reqs.size(), p->tree.reqs.data(), false, mass, mass_cap, st, "sled_tree_mass")) != SLED_OK) return rc;
-    for (int r : p->tree.reqs) p->reqs[r].mass_added = true;
+    if (!p->reqs[p->tree.reqs[0]].mass_noted) {   // (the plan's requests are opened together)
+        std::vector<int> nodes;
+        for (int r : p->tree.reqs) nodes.push_back(p->reqs[r].staged);
+        if ((rc = open_mass(p, (int)nodes.size(), p->tree.reqs.data(), nodes.data(), false, mass, mass_cap, st, "sled_tree_mass")) != SLED_OK) return rc;
+    }
     return sled_launch_tree_mass(m, p, p->tree.plan, layer, q, q_stride, 0, lse, mass, mass_cap, st);
 }
 SLED_CATCH("sled_tree_mass")
@@ -1643,7 +1665,7 @@ extern "C" int sled_tree_commit(sled_kvpool* p, int B, const int* req_ids, const
         if (mass && (rc = check_mass(p, mass_cap, rq.len_ub + rq.staged, "sled_tree_commit")) != SLED_OK) return rc;
         need += rq.pages.size();
     }
-    if (mass && (rc = clear_mass(p, B, req_ids, false, mass, mass_cap, st, "sled_tree_commit")) != SLED_OK) return rc;
+    if (mass && (rc = open_mass(p, B, req_ids, nullptr, false, mass, mass_cap, st, "sled_tree_commit")) != SLED_OK) return rc;
     sled_stage_slot* sl;
     if ((rc = stage_acquire(p, need, &sl)) != SLED_OK) return rc;
     size_t off = 3 * (size_t)B;
@@ -1693,10 +1715,7 @@ extern "C" int sled_verify_tree(sled_model* m, sled_kvpool* p, int B, const int*
     if ((rc = plan_trees(p, B, req_ids, n_nodes, parent, ws + w.plan, workspace_bytes - w.plan, st, "sled_verify_tree")) != SLED_OK) return rc;
     p->tree.valid = false;   // (the plan serves this step alone)
     for (int i = 0; i < B; i++) p->reqs[req_ids[i]].staged = -1;   // nothing to commit until all of it is on its way
-    if (mass) {
-        if ((rc = clear_mass(p, B, req_ids, false, mass, mass_cap, st, "sled_verify_tree")) != SLED_OK) return rc;
-        for (int i = 0; i < B; i++) p->reqs[req_ids[i]].mass_added = true;
-    }
+    if (mass && (rc = open_mass(p, B, req_ids, n_nodes, false, mass, mass_cap, st, "sled_verify_tree")) != SLED_OK) return rc;
     std::vector<step_entry> ent(B);
     for (int i = 0; i < B; i++) ent[i] = step_entry{req_ids[i], 0, n_nodes[i]};
     const tree_step tr{&p->tree.plan, depth.data(), ws + w.k, ws + w.v, reinterpret_cast<float*>(ws + w.lse), mass, mass_cap};
@@ -1766,8 +1785,8 @@ extern "C" int sled_kv_evict(sled_kvpool* p, int B, const int* req_ids, const in
     if (idx_bytes > workspace_bytes) SLED_FAIL(SLED_EINVAL, "sled_kv_evict: workspace of %zu bytes, %zu needed", workspace_bytes, idx_bytes);
     if ((rc = reset_fresh_lengths(p, B, req_ids, st)) != SLED_OK) return rc;
     if (!in_place && (rc = reset_fresh_lengths(p, B, dst_ids, st)) != SLED_OK) return rc;
-    if ((rc = clear_mass(p, B, req_ids, in_place, mass, mass_cap, st, "sled_kv_evict")) != SLED_OK) return rc;
-    if (!in_place && (rc = clear_mass(p, B, dst_ids, false, mass, mass_cap, st, "sled_kv_evict")) != SLED_OK) return rc;
+    if ((rc = open_mass(p, B, req_ids, nullptr, in_place, mass, mass_cap, st, "sled_kv_evict")) != SLED_OK) return rc;
+    if (!in_place && (rc = open_mass(p, B, dst_ids, nullptr, false, mass, mass_cap, st, "sled_kv_evict")) != SLED_OK) return rc;
     size_t need = (size_t)SLED_EVICT_REC * B;
     for (int i = 0; i < B; i++) {
         const int src_ub = p->reqs[req_ids[i]].len_ub;

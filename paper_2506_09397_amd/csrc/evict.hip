@@ -364,12 +364,14 @@ __global__ __launch_bounds__(64) void tree_len_kernel(commit_args a) {
     if (a.mass && lane < 2) a.tail[2 * rec[0] + lane] = 0;
 }
 
-// What nodes that were dropped have left behind, a workgroup per request: up to 64 slots of every layer and head.
-__global__ __launch_bounds__(256) void mass_clear_kernel(sled_some_ids ids, int32_t* __restrict__ tail, float* __restrict__ mass, int cap, int n_lh) {
-    const int r = ids.id[blockIdx.x], from = tail[2 * r], n = min(tail[2 * r + 1], cap) - from;
+// Once before a step's nodes get mass, or where mass is read: what nodes that were dropped have left behind goes (up to 64 slots of every layer and
+// head), and where those of the step lie is noted.  A workgroup per request.
+__global__ __launch_bounds__(256) void mass_open_kernel(sled_mass_ids ids, const int32_t* __restrict__ len_dev, int32_t* __restrict__ tail, float* __restrict__ mass,
+                                                        int cap, int n_lh) {
+    const int r = ids.id[blockIdx.x], nodes = ids.nodes[blockIdx.x], from = tail[2 * r], n = ids.left[blockIdx.x] ? min(tail[2 * r + 1], cap) - from : 0;
     for (int i = threadIdx.x; i < n_lh * n; i += 256) mass[((size_t)r * n_lh + i / n) * cap + from + i % n] = 0.f;
     __syncthreads();
-    if (threadIdx.x < 2) tail[2 * r + threadIdx.x] = 0;
+    if (threadIdx.x < 2) tail[2 * r + threadIdx.x] = nodes ? len_dev[r] + threadIdx.x * nodes : 0;
 }
 
 template <int D, bool F32>
@@ -403,14 +405,9 @@ int sled_launch_evict(const sled_model* m, const sled_kvpool* p, const int32_t* 
     return SLED_OK;
 }
 
-int sled_launch_mass_clear(const sled_model* m, const sled_kvpool* p, const int* req_ids, int n, float* mass, int cap, hipStream_t st) {
-    for (int i0 = 0; i0 < n; i0 += 128) {
-        sled_some_ids ids{};
-        const int here = std::min(n - i0, 128);
-        for (int i = 0; i < here; i++) ids.id[i] = req_ids[i0 + i];
-        hipLaunchKernelGGL(mass_clear_kernel, dim3(here), dim3(256), 0, st, ids, p->tail_dev, mass, cap, m->s.n_layers * m->s.n_kv_heads);
-        SLED_LAUNCH_CHECK();
-    }
+int sled_launch_mass_open(const sled_model* m, const sled_kvpool* p, const sled_mass_ids& ids, int n, float* mass, int cap, hipStream_t st) {
+    hipLaunchKernelGGL(mass_open_kernel, dim3(n), dim3(256), 0, st, ids, p->len_dev, p->tail_dev, mass, cap, m->s.n_layers * m->s.n_kv_heads);
+    SLED_LAUNCH_CHECK();
     return SLED_OK;
 }
 

@@ -594,7 +594,10 @@ __global__ void len_add_kernel(int32_t* __restrict__ len_dev, int32_t* __restric
     len_dev[r] = from + (accept ? accept[i] + 1 : add[i]);
 }
 // the lengths (and positions) of requests that have just been opened, up to 128 in a launch
-__global__ void len_zero_kernel(int32_t* __restrict__ len_dev, int32_t* __restrict__ shift_dev, int32_t* __restrict__ tail_dev, sled_some_ids ids, int n) {
+struct len_ids {
+    int id[128];
+};
+__global__ void len_zero_kernel(int32_t* __restrict__ len_dev, int32_t* __restrict__ shift_dev, int32_t* __restrict__ tail_dev, len_ids ids, int n) {
     if ((int)threadIdx.x >= n) return;
     const int r = ids.id[threadIdx.x];
     len_dev[r] = shift_dev[r] = tail_dev[2 * r] = tail_dev[2 * r + 1] = 0;
@@ -860,7 +863,7 @@ int sled_launch_len_add(const sled_kvpool* p, const int32_t* req_ids_dev, const 
 
 int sled_launch_len_zero(const sled_kvpool* p, const int* req_ids /*host*/, int n, hipStream_t st) {
     for (int i0 = 0; i0 < n; i0 += 128) {
-        sled_some_ids ids{};
+        len_ids ids{};
         const int here = std::min(n - i0, 128);
         for (int i = 0; i < here; i++) ids.id[i] = req_ids[i0 + i];
         hipLaunchKernelGGL(len_zero_kernel, dim3(1), dim3(128), 0, st, p->len_dev, p->shift_dev, p->tail_dev, ids, here);

@@ -169,6 +169,7 @@ struct sled_request {
     int len_ub = 0;            // host-side upper bound of the committed length
     int staged = -1;           // k+1 of the last verify (rows staged), -1 if none
     bool mass_added = false;   // the staged tree's nodes have mass in their slots (sled_tree_mass)
+    bool mass_noted = false;   // ... and tail_dev says where (a captured call has only promised so)
     bool mass_left = false;    // a tree's nodes that were dropped since have: cleared by the next call that is given mass (tail_dev says where)
     int64_t added = 0;         // everything ever added to len_ub (lets a late read-back of the exact length be applied)
     uint32_t gen = 0;          // incarnation of the slot: a read-back taken for an earlier one is dropped
@@ -319,14 +320,15 @@ int sled_launch_tree_qkv(const sled_model* m, int T, const float* partial, int n
 constexpr int SLED_EVICT_REC = 5;
 int sled_launch_evict(const sled_model* m, const sled_kvpool* p, const int32_t* meta, const int32_t* pages, int B, int keep_max, int first, int recent, float* mass,
                       int cap, int32_t* idx, int idx_cap, bool in_place, hipStream_t st);
-int sled_launch_mass_clear(const sled_model* m, const sled_kvpool* p, const int* req_ids /*host*/, int n, float* mass, int cap, hipStream_t st);
+// requests of a launch that takes them by value: the nodes that are to get mass (0: none), whether dropped ones have left some
+constexpr int SLED_MASS_IDS = 128;
+struct sled_mass_ids {
+    int id[SLED_MASS_IDS];
+    uint8_t nodes[SLED_MASS_IDS], left[SLED_MASS_IDS];
+};
+int sled_launch_mass_open(const sled_model* m, const sled_kvpool* p, const sled_mass_ids& ids, int n, float* mass, int cap, hipStream_t st);
 int sled_launch_tree_commit(const sled_model* m, const sled_kvpool* p, const int32_t* meta, const int32_t* pages, int B, const int32_t* accept_len,
                             const int32_t* path, float* mass, int cap, hipStream_t st);
-
-// ids of a launch that takes them by value
-struct sled_some_ids {
-    int id[128];
-};
 
 // accept_tree.hip
 size_t sled_accept_tree_ws_bytes(int B, int T, int vocab);

@@ -793,7 +793,6 @@ __host__ __device__ constexpr int mass_rows(int PL) { return PL == 1 ? 256 : 128
 struct mass_args {
     float* mass;   // [request][layer][kv head][cap]
     int cap, n_layers;
-    int32_t* tail; // [request][2] where its nodes' mass lies, should they be dropped
 };
 
 // (two workgroups a CU where the registers allow it)
@@ -808,7 +807,6 @@ __global__ __launch_bounds__(64 * MASS_WAVES, PL == 1 && !F32 ? 4 : 2) void tree
     const int L = a.len_dev[req], G = a.Hq / a.Hkv, rows = G * n;
     const int page_end = min(page0 + npg, (L + n + 15) >> 4);
     if (page0 >= page_end) return;
-    if (page0 == 0 && g == 0 && tid < 2) ma.tail[2 * req + tid] = tid ? L + n : L;
     const int lr = lane & 15, lg = lane >> 4;
     u32x4* qs = reinterpret_cast<u32x4*>(smem);
     const int room = min(MR, (rows + 15) & ~15);
@@ -1035,7 +1033,7 @@ int sled_launch_tree_mass(const sled_model* m, const sled_kvpool* p, const sled_
                           const float* lse, float* mass, int cap, hipStream_t st) {
     tree_args a = common_args(m, p, t, layer, q, q_stride, q_plane);
     a.lse = const_cast<float*>(lse);
-    const mass_args ma{mass, cap, m->s.n_layers, p->tail_dev};
+    const mass_args ma{mass, cap, m->s.n_layers};
     const int rows = t.max_nodes * (m->s.n_q_heads / m->s.n_kv_heads);
     if (m->s.dtype == SLED_BF16) return q_plane ? launch_mass<128, false, 2>(a, ma, rows, st) : launch_mass<128, false, 1>(a, ma, rows, st);
     return m->s.head_dim == 64 ? launch_mass<64, true, 1>(a, ma, rows, st) : launch_mass<128, true, 1>(a, ma, rows, st);

@@ -215,6 +215,33 @@ def test_a_captured_call_does_not_clear():
         assert bool((t.mass[t.reqs[0], :, :, 43:] == 0).all())
 
 
+@pytest.mark.parametrize("first", ["replayed", "eager"])
+def test_a_plan_whose_first_mass_is_captured(first):
+    """Whether the graph runs or an eager call takes its place, a dropped tree leaves nothing."""
+    with pool(*HEADS["8b"], layers=LAYERS) as p:
+        t = Steps(p, [40, 17], seed=8)
+        t.begin([30, 9])
+        t.layers(with_mass=False)
+        torch.cuda.synchronize()
+
+        def add():
+            for l in range(LAYERS):
+                sled.sled_tree_mass(p.pool, l, t.q[l], t.lse[l], t.mass, t.ws)
+
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            add()
+        assert bool((t.mass == 0).all())
+        graph.replay() if first == "replayed" else add()
+        torch.cuda.synchronize()
+        once = [t.exact(i) for i in range(2)]
+        t.step([3, 2])
+        for i, (L, n) in enumerate(zip([40, 17], [3, 2])):
+            got, second = t.mass[t.reqs[i]], t.exact(i)
+            close(got[..., :L + n], torch.cat([once[i][..., :L] + second[..., :L], second[..., L:]], dim=2))
+            assert bool((got[..., L + n:] == 0).all())
+
+
 @pytest.mark.parametrize("dropped_by", ["prefill", "chain"])
 def test_prompts_and_chains_in_a_dropped_trees_place(dropped_by):
     """Two requests with the same tokens and caches, one of which had a tree with mass in between: the next step gives both the same mass."""
