@@ -20,6 +20,7 @@ class Verifier:
             sled.sled_model_set_batch_invariant(self.model, True)   # before the workspace is sized
         sled.load_weights(self.model, weights)
         self.pool = sled.sled_kvpool_create(self.model, n_pages, max_requests)
+        self.max_requests = max_requests
         self.T_max = B_max * (shape.k_max + 1)
         self.B_max = B_max
         self.ws = sled.workspace(sled.sled_verify_workspace_bytes(self.model, B_max, self.T_max, ctx_tokens_max))
@@ -82,8 +83,10 @@ class Verifier:
     # ---- trees of drafts, a bounded cache -----------------------------------------------------
     def enable_trees(self, nodes_max: int, ctx_tokens_max: int, mass_cap: int = 0, max_requests: int = 0) -> None:
         """Buffers for steps over trees of up to nodes_max nodes on contexts of ctx_tokens_max tokens together.  mass_cap > 0: the weight that
-        attention gives the tokens of up to max_requests requests of up to mass_cap tokens (nodes included) is added up, for evict()."""
-        s, B = self.shape, self.B_max
+        attention gives the tokens of requests of up to mass_cap tokens (nodes included) is added up, for evict(); max_requests is the pool's own number, or
+        0 for that."""
+        s, B, max_requests = self.shape, self.B_max, max_requests or self.max_requests
+        assert max_requests >= self.max_requests, "a row of mass for every request of the pool"
         self.nodes_max = min(nodes_max, sled.TREE_MAX)
         T = B * self.nodes_max
         self.tree_ws = sled.workspace(sled.sled_verify_tree_workspace_bytes(self.model, B, T, ctx_tokens_max + T))

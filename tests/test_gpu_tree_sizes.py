@@ -58,3 +58,16 @@ def test_a_device_that_drafts_more_than_the_verifier_holds():
     assert [r.device for r in answers] == [0, 1, 2]
     assert v.lengths([server.req_of[d] for d in range(3)]) == [10 + d + r.accept_len + 1 for d, r in enumerate(answers)]
     v.destroy()
+
+
+def test_mass_for_all_requests_of_the_pool_unless_said_otherwise():
+    shape = synth.SHAPES["tiny_bf16"]
+    v = Verifier(shape, synth.SynthWeights(shape, seed=1, device="cuda"), 40, 5, 2, 200)
+    with pytest.raises(AssertionError, match="every request"):
+        v.enable_trees(6, 100, mass_cap=50, max_requests=4)
+    v.enable_trees(6, 100, mass_cap=50)
+    assert v.mass.shape[0] == 5
+    r = v.open_bounded()
+    v.verify_tree([r], [[-1, 0, 0]], torch.zeros(3, dtype=torch.int32, device="cuda"))
+    assert abs(float(v.mass[r].sum()) - shape.n_layers * 3 * shape.n_q_heads) < 1e-2     # a weight of one a row, head and layer
+    v.destroy()
