@@ -148,6 +148,8 @@ class Server:
             if round_no < last.round_no:
                 raise ValueError(f"device {device}: round {round_no} is older than the last answered round {last.round_no}")
             return dataclasses.replace(last, replayed=True)
+        if not all(-(2**31) <= int(t) < 2**31 for t in (pending_token, *drafts)):   # (ids outside the vocabulary are clamped by the step)
+            raise ValueError(f"device {device}: a token id that 32 bits do not hold")
         if self.trees:
             # (like a chain's: what the verifier's buffers do not hold is drafted again; a node comes behind the one it continues, so a front part is a tree)
             drafts = [int(d) for d in drafts][: min(sled.TREE_MAX, getattr(self.v, "nodes_max", sled.TREE_MAX)) - 1]

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2506_09397_amd import serving
-from test_serving_host import toy_truth
+from test_serving_host import ToyVerifier, toy_truth
 from test_serving_trees_host import ToyTrees
 
 
@@ -42,3 +42,18 @@ def test_a_verifier_without_a_limit_takes_the_largest_trees():
     t = toy_truth([5], 80)
     s.submit(0, 0, 5, t[:70])
     assert s.run_batch()[0].accept_len == 63
+
+
+@pytest.mark.parametrize("trees", [False, True])
+def test_token_ids_that_no_step_can_take_are_refused_where_they_come_in(trees):
+    """... and not when the batch they are in has left the queue."""
+    s = serving.Server(ToyTrees() if trees else ToyVerifier(), 2, device="cpu", trees=trees)
+    for d in range(2):
+        s.open(d)
+    t = toy_truth([5], 3)
+    s.submit(0, 0, 5, t[:2])
+    for pending, drafts in ((5, [1, 2**31]), (5, [-(2**31) - 1]), (2**40, [])):
+        with pytest.raises(ValueError, match="32 bits"):
+            s.submit(1, 0, pending, drafts)
+    s.submit(1, 0, 5, [t[0]])
+    assert [r.accept_len for r in s.run_batch()] == [2, 1]
