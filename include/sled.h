@@ -361,9 +361,9 @@ SLED_API size_t sled_tree_workspace_bytes(const sled_model* m, int B_max, int T_
  *   workspace                          dev scratch, 256-byte aligned; the plan lives in it until the requests' next
  *                                      commit, append, verify, prefill, eviction or close, or the pool's next
  *                                      sled_tree_begin or sled_verify_tree
- * What an earlier step staged for these requests is dropped.  Cannot be captured into a graph (the calls that use the
- * plan, sled_tree_attention and sled_tree_mass, can; replays then use the plan the workspace holds at that time, on
- * unchanged requests).
+ * What an earlier step staged for these requests is dropped.  Cannot be captured into a graph.  The calls that use the plan,
+ * sled_tree_attention and sled_tree_mass, can; their launches hold the plan's sizes and its places in the workspace, so they
+ * may be replayed, with new inputs in the same buffers, as long as that plan lives and not after another sled_tree_begin.
  * Errors: SLED_EINVAL (bad tree, unknown or duplicate request, small workspace), SLED_ENOMEM, SLED_ESTATE (capture). */
 SLED_API int sled_tree_begin(sled_kvpool* p, int B, const int* req_ids /*host*/, const int* n_nodes /*host*/, const int* parent /*host*/,
                     void* workspace /*dev*/, size_t workspace_bytes, void* stream);
