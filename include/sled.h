@@ -31,7 +31,9 @@
  *     are ordinary host memory, read before the call returns.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All device
  *     work is enqueued on it and the calls return without waiting for it, except where
- *     stated.  Calls that touch the same pool must be issued on one stream or be ordered
+ *     stated and where a pool's staging of metadata is short: a call with more of it (page
+ *     lists, work items) than any before on its pool makes the buffers grow, and one that
+ *     is far ahead of the device waits for a buffer, both for earlier work.  Calls that touch the same pool must be issued on one stream or be ordered
  *     by the caller.
  *   - The library owns what sits behind its handles: packed weights, the paged K/V pool.
  *   - Handles are not thread-safe; use one thread per handle or lock outside.
@@ -383,7 +385,9 @@ SLED_API int sled_tree_attention(sled_kvpool* p, int layer, const void* q /*dev*
                         void* workspace /*dev*/, void* stream);
 
 /* Adds up what weight each cached token got on one layer: mass[token] += sum over the nodes of the request's tree and the query
- * heads of a kv head of softmax(q K^T / sqrt(head_dim))[token].  For sled_kv_evict.  Comes after sled_tree_attention of that layer,
+ * heads of a kv head of softmax(q K^T / sqrt(head_dim))[token].  For sled_kv_evict.  The rows of all nodes count, also of those that
+ * are not accepted then: a tree of many wrong guesses has that much more say in what stays.  Prompts and chain steps add nothing, so a
+ * prompt's tokens start from zero and the first eviction after it goes by the rows of the trees since.  Comes after sled_tree_attention of that layer,
  * with its q and the lse it returned.
  *   mass  dev float32 [max_requests][n_layers][n_kv_heads][mass_cap], the row of a request by its id; mass_cap at least the
  *         library's bound of L_i + n_i; one array for a pool.  Zero a request's rows when it is opened.  A node's own slot gets its mass

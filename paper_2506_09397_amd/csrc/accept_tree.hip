@@ -9,7 +9,8 @@
 //               in what that left, 1 us a node (greedy) or 8 (sampling: the piece in which the sum passes is gone through once more).
 //   many rows   one launch: a workgroup of 16 wavefronts walks for a request and goes through each row by itself, with up to 256 KB asked for at a
 //               time: 8 us a row of 128256 values out of L2, 14 out of memory; by sampling 22 us a row of 50257, one CU's float64 exponentials.
-// 16 trees of 333 nodes, 128256 values, up to 6 accepted: 37 us; 64 trees of 1946 nodes by sampling, 50257 values, up to 7 accepted: 190 us.  A launch per
+// 16 trees of 333 nodes, 128256 values, up to 6 accepted: 38 us; 64 trees of 1946 nodes by sampling, 50257 values, up to 7 accepted: 172 to 217 us by the
+// longest walk.  A launch per
 // level of the trees took 86 and 288 us: it has to launch for the deepest tree, whose last nodes are hardly ever reached.
 // Sums of exponentials are float64 in a fixed order over the row: what rounding leaves between the forms is 1e-14 of the sum.
 #include "sled_internal.h"

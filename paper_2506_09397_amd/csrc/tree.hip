@@ -879,6 +879,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES, PL == 1 && !F32 ? 4 : 2) void tree
                         float sum = 0.f;
 #pragma unroll
                         for (int i = 0; i < 4; i++) {
+                            // (the denominator's logarithm in log2 units is off by 2^-24 of itself: by no more than the score's own sum)
                             float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -zz[i]));
                             if (decltype(masked)::value) {
                                 const int c = (p0 + p) * 16 + lr - L;   // node of this lane's token, if not context
