@@ -481,6 +481,12 @@ static void trim_pages(sled_kvpool* p, sled_request& rq) {
     }
 }
 
+// a call that is refused gives back what it has reserved so far
+static int refuse(sled_kvpool* p, int B, const int* req_ids, int rc) {
+    for (int i = 0; i < B; i++) trim_pages(p, p->reqs[req_ids[i]]);
+    return rc;
+}
+
 // Applies every length read-back whose copy has completed (never waits): the exact length L of a request right after
 // some commit, plus whatever has been added to its bound since, is a tighter bound than the one kept so far.
 static void poll_readbacks(sled_kvpool* p) {
@@ -1410,7 +1416,7 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
     std::vector<tree_group> groups;
     for (int i = 0; i < B; i++) {
         const sled_request& rq = p->reqs[req_ids[i]];
-        if ((rc = ensure_pages(p, req_ids[i], rq.len_ub + n_nodes[i])) != SLED_OK) return rc;
+        if ((rc = ensure_pages(p, req_ids[i], rq.len_ub + n_nodes[i])) != SLED_OK) return refuse(p, B, req_ids, rc);
         np[i] = ceil_div(rq.len_ub, 16);
         n_pages += ceil_div(rq.len_ub + n_nodes[i], 16);
         reach_max = std::max(reach_max, rq.len_ub + n_nodes[i]);
@@ -1440,7 +1446,10 @@ int plan_trees(sled_kvpool* p, int B, const int* req_ids, const int* n_nodes, co
     }
     for (int i = 0; i < B; i++) n_mass += (int64_t)Hkv * ceil_div(ceil_div(p->reqs[req_ids[i]].len_ub + n_nodes[i], 16), (int)mass_chunk);
     const tree_layout w = tree_plan_layout(m, n_items, n_slots, n_mass, T, n_pages);
-    if (w.total > workspace_bytes) SLED_FAIL(SLED_EINVAL, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, w.total);
+    if (w.total > workspace_bytes) {
+        sled_set_error("%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, w.total);
+        return refuse(p, B, req_ids, SLED_EINVAL);
+    }
     sled_stage_slot* sl;
     if ((rc = stage_acquire(p, w.ints / 4, &sl)) != SLED_OK) return rc;
     char* host = reinterpret_cast<char*>(sl->host);
@@ -1790,7 +1799,7 @@ extern "C" int sled_kv_evict(sled_kvpool* p, int B, const int* req_ids, const in
     size_t need = (size_t)SLED_EVICT_REC * B;
     for (int i = 0; i < B; i++) {
         const int src_ub = p->reqs[req_ids[i]].len_ub;
-        if (!in_place && (rc = ensure_pages(p, dst_ids[i], std::min(keep[i], src_ub))) != SLED_OK) return rc;
+        if (!in_place && (rc = ensure_pages(p, dst_ids[i], std::min(keep[i], src_ub))) != SLED_OK) return refuse(p, B, dst_ids, rc);
         need += p->reqs[req_ids[i]].pages.size() + (in_place ? 0 : p->reqs[dst_ids[i]].pages.size());
     }
     sled_stage_slot* sl;
