@@ -33,8 +33,8 @@
  *     work is enqueued on it and the calls return without waiting for it, except where
  *     stated and where a pool's staging of metadata is short: a call with more of it (page
  *     lists, work items) than any before on its pool makes the buffers grow, and one that
- *     is far ahead of the device waits for a buffer, both for earlier work.  Calls that touch the same pool must be issued on one stream or be ordered
- *     by the caller.
+ *     is far ahead of the device waits for a buffer, both for earlier work.  Calls that
+ *     touch the same pool must be issued on one stream or be ordered by the caller.
  *   - The library owns what sits behind its handles: packed weights, the paged K/V pool.
  *   - Handles are not thread-safe; use one thread per handle or lock outside.
  *
@@ -379,7 +379,8 @@ SLED_API int sled_tree_begin(sled_kvpool* p, int B, const int* req_ids /*host*/,
  * Softmax and sums in float32; a bf16 model's weights enter the product with V with 16 significant bits, the result is
  * rounded once.  Keys and values of a node do not reach nodes that do not see it, not even where they are not finite.
  * out and lse must not overlap the inputs.  Results do not depend on the other requests of the batch but for the order of float32 sums over split contexts
- * (not even that for batch-invariant models, nor whether the exact lengths of an earlier commit have arrived).  Errors: SLED_EINVAL, SLED_ESTATE (no plan). */
+ * (batch-invariant models: not even that, and not on whether an earlier commit's exact lengths have arrived).
+ * Errors: SLED_EINVAL, SLED_ESTATE (no plan). */
 SLED_API int sled_tree_attention(sled_kvpool* p, int layer, const void* q /*dev*/, int64_t q_stride, const void* k /*dev*/, int64_t k_stride,
                         const void* v /*dev*/, int64_t v_stride, void* out /*dev out*/, float* lse /*dev out or NULL*/,
                         void* workspace /*dev*/, void* stream);

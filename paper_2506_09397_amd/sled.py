@@ -154,7 +154,7 @@ class _PoolInfo:
 
     def plan(self, rows: int) -> None:
         """The trees that sled_tree_begin has planned last have so many nodes (0: none so far, the library refuses what comes)."""
-        self.rows, self.q, self.kv, self.lse = rows, (rows, *self.q_row), (rows, *self.kv_row), (rows, self.q_row[0])
+        self.rows, self.q, self.kv = rows, (rows, *self.q_row), (rows, *self.kv_row)
 
 
 _models: Dict[int, ModelShape] = {}
@@ -185,7 +185,8 @@ def sled_model_destroy(model: int) -> None:
 def sled_kvpool_create(model: int, n_pages: int, max_requests: int) -> int:
     h = C.c_void_p()
     _check(lib().sled_kvpool_create(model, n_pages, max_requests, C.byref(h)))
-    _pools[h.value] = _PoolInfo(_models[model], max_requests)
+    if model in _models:
+        _pools[h.value] = _PoolInfo(_models[model], max_requests)
     return h.value
 
 
