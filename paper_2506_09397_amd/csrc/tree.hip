@@ -879,7 +879,9 @@ __global__ __launch_bounds__(64 * MASS_WAVES, PL == 1 && !F32 ? 4 : 2) void tree
                         float sum = 0.f;
 #pragma unroll
                         for (int i = 0; i < 4; i++) {
-                            // (the denominator's logarithm in log2 units is off by 2^-24 of itself: by no more than the score's own sum)
+                            // (scale and denominator in log2 units are off by half a step of 2^-23 of themselves, as the score's own sum is: 3e-8 to
+                            // 1.7e-7 of the masses of 14 batches together, 3e-8 to 7e-8 where lse itself is taken off.  That would be one more
+                            // instruction for each of a tile's elements, which are what the kernel is bound by)
                             float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -zz[i]));
                             if (decltype(masked)::value) {
                                 const int c = (p0 + p) * 16 + lr - L;   // node of this lane's token, if not context
